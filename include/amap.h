@@ -418,11 +418,108 @@ amap_status amap_gemm_mapped(const void *A_src, const amap_t *A_map, const void 
 amap_status amap_gemm_gather(const void *const *A_srcs, const amap_t *A_map, const void *W_src, const amap_t *W_map,
                              int64_t N, const amap_t *out_map, void *out, void *stream);
 
+/* ---- a paged key-value cache (device pointers; asynchronous on `stream`) ---
+ * Keys and values of many requests in pages of page_size tokens: an access map whose outermost digit
+ * is known on the device only.  Token i of request r lies in page table[r, i / page_size], row
+ * i % page_size; slot = page * page_size + row names a place in the cache by itself.  A decoder step is
+ * amap_cache_assign (pages for the step's tokens, their slots and positions), the product that gives q, k
+ * and v, amap_cache_append (k and v stored, k and q turned to their positions), amap_cache_attend, and the
+ * product that reads the heads (amap_gemm_fused).  Unlike in a layout chain elements have a type here.
+ * No call allocates, synchronises, or reads device memory on the host; what the device finds out of
+ * range (a slot or page outside the cache, a negative length) is left out, as said at each call, and never
+ * addressed.  Refusals: AMAP_E_INVALID (null pointers, types, negative sizes), AMAP_E_SHAPE (sizes that do not
+ * fit one another, outputs whose elements overlap), AMAP_E_ALIAS, AMAP_E_UNSUPPORTED (amap_last_error says what). */
+
+typedef enum { AMAP_F32 = 0, AMAP_BF16 = 1, AMAP_F16 = 2, AMAP_E4M3 = 3 /* OCP 8-bit float, up to 448 */ } amap_type;
+
+/* A [tokens, heads, head_dim] tensor; strides in elements, the elements of a head side by side. */
+typedef struct {
+    void *data;
+    amap_type type;
+    int heads;
+    int64_t token_stride, head_stride;
+} amap_heads;
+
+/* Rotary positions.  Pair p of a head is its elements (p, p + pairs), or (2p, 2p + 1) where interleaved; elements
+ * from 2 * pairs on are left as they are.  The first axis_pairs[0] pairs belong to axis 0, the next
+ * axis_pairs[1] to axis 1, and so on (time, height, width); pair p of a token is turned by the angle
+ * position[axis] * freq[p], taken in 64 bits: (a, b) -> (a cos - b sin, b cos + a sin). */
+#define AMAP_MAX_AXES 4
+typedef struct {
+    const float *freq;          /* [pairs], device */
+    int pairs;
+    int interleaved;
+    int n_axes;
+    int32_t axis_pairs[AMAP_MAX_AXES];   /* sum = pairs */
+} amap_rope;
+
+/* The cache.  Strides in elements, the same for keys and values; [pages, page_size, kv_heads, head_dim],
+ * [pages, kv_heads, page_size, head_dim] and any other order with the elements of a head side by side.
+ * E4M3: an element stands for its value times the scale of its head (scales NULL: 1). */
+typedef struct {
+    void *k, *v;
+    amap_type type;             /* AMAP_BF16, AMAP_F16, AMAP_E4M3 */
+    int64_t n_pages;
+    int page_size, kv_heads, head_dim;
+    int64_t page_stride, token_stride, head_stride;
+    const float *k_scale, *v_scale;      /* [kv_heads], device; E4M3 only */
+} amap_cache;
+
+/* Block tables and slot maps of a step, from request lengths.  Request r has cached[r] tokens in its pages
+ * (NULL: none) and adds fresh[r] of them.  The pages that takes are handed out from free_pages in the order of the
+ * requests: entries [ceil(cached / page_size), ceil((cached + fresh) / page_size)) of row r of the table, as
+ * far as the table is wide; the table's other entries are neither read nor written but those of pages that fresh tokens go on in.  The
+ * step's tokens, request after request, get their owner, position cached + i and slot; a token without a page (the list or
+ * the table's row at its end, or an entry that is no page: < 0) gets slot -1, and everything from the last token
+ * to n_tokens -1.  All arrays are int32 but slot.  `cached` and `table` may be read again: the same call gives the same.
+ * requests <= 16384; sums of tokens under 2^31.  Negative lengths count as 0. */
+typedef struct {
+    int64_t requests;
+    int page_size;
+    const int32_t *cached, *fresh;       /* [requests] */
+    const int32_t *free_pages;
+    int64_t n_free;
+    int32_t *table;                      /* [requests, table_width], rows table_stride apart */
+    int64_t table_stride;
+    int table_width;
+    int32_t *begin;                      /* [requests + 1]: where each request's fresh tokens begin */
+    int32_t *length;                     /* [requests]: cached + fresh */
+    int64_t *slot;                       /* [n_tokens] */
+    int32_t *position, *owner;           /* [n_tokens] */
+    int64_t n_tokens;
+    int32_t *taken;                      /* [1]: pages that the step needs from the list (more than n_free: it was short) */
+} amap_assign;
+amap_status amap_cache_assign(const amap_assign *a, void *stream);
+
+/* out = x with every pair turned (inverse: turned back, which is the gradient of the turn as well).  x and out have the
+ * same type (F32, BF16, F16) and heads; out is x itself or does not overlap it.  Axis a of token t is at
+ * position[a * axis_stride + t] (axis_stride 0: the same for all). */
+amap_status amap_rotary(const amap_heads *x, const amap_heads *out, int64_t tokens, int head_dim, const amap_rope *rope,
+                        const int32_t *position, int64_t axis_stride, int inverse, void *stream);
+
+/* k and v of `tokens` tokens into the cache at their slots, rounded once to its type (E4M3: divided by the
+ * head's scale, at most 448 either way).  Slots outside the cache are left out; no slot may come twice.  With a rope
+ * (NULL: none) k is turned on the way, and q (NULL: none) into q_out as by amap_rotary, out of the cache's way. */
+amap_status amap_cache_append(const amap_cache *cache, const amap_heads *k, const amap_heads *v, int64_t tokens, const int64_t *slot,
+                              const amap_rope *rope, const int32_t *position, int64_t axis_stride, const amap_heads *q,
+                              const amap_heads *q_out, void *stream);
+
+/* Attention of one new token per request over its cache: s_i = scale q . k_i over the tokens i < length[r] (window > 0: the last
+ * `window` of them) whose page lies in the cache, out = sum softmax(s)_i v_i, lse (may be NULL) = log sum exp s_i, [requests, heads] row
+ * by row.  A row that sees no token, or whose scores are all -inf, is 0 with lse -inf.  Heads heads / kv_heads * h .. share key head h.  What lies in
+ * the cache outside the visible tokens is never used, whatever it holds.  A length beyond the table's width counts as
+ * that.  q and out: BF16 or F16 alike; head_dim a multiple of 8 (E4M3: 16) up to 256, rows of the cache 16-byte aligned.
+ * workspace: amap_cache_attend_workspace bytes, 16-byte aligned; its contents need not be kept. */
+amap_status amap_cache_attend(const amap_cache *cache, const amap_heads *q, int64_t requests, const int32_t *table, int64_t table_stride,
+                              int table_width, const int32_t *length, float scale, int window, const amap_heads *out, float *lse,
+                              void *workspace, int64_t workspace_bytes, void *stream);
+amap_status amap_cache_attend_workspace(const amap_cache *cache, int heads, int64_t requests, int table_width, int64_t *bytes);
+
 const char *amap_status_str(amap_status s);
 
 /* Text of the HIP error behind the last AMAP_E_HIP returned on this thread, or the reason
- * why a device entry point (amap_execute*, amap_gemm_*) last returned AMAP_E_UNSUPPORTED on
- * this thread (which requirement the maps did not meet); empty string if none. */
+ * why a device entry point (amap_execute*, amap_gemm_*, amap_cache_*, amap_rotary) last returned AMAP_E_UNSUPPORTED
+ * on this thread (which requirement the arguments did not meet); empty string if none. */
 const char *amap_last_error(void);
 
 #ifdef __cplusplus

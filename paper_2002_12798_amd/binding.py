@@ -25,6 +25,8 @@ AMAP_TRANSPOSE, AMAP_RESHAPE, AMAP_SLICE, AMAP_PAD, AMAP_CONCAT, AMAP_REPEAT, AM
 AMAP_K_PROGRAM, AMAP_K_ELEMENT, AMAP_K_ROWS, AMAP_K_TILE, AMAP_K_WAVE = range(5)
 KERNEL_NAMES = {0: "program", 1: "element", 2: "rows", 3: "tile", 4: "wave"}
 AMAP_MAX_RANK = 8
+AMAP_F32, AMAP_BF16, AMAP_F16, AMAP_E4M3 = range(4)
+AMAP_MAX_AXES = 4
 
 EXPORTS = [
     "amap_source", "amap_transpose", "amap_reshape", "amap_slice", "amap_repeat", "amap_tile", "amap_pad",
@@ -37,6 +39,7 @@ EXPORTS = [
     "amap_graph_output", "amap_graph_eliminate", "amap_graph_load",
     "amap_layout_create", "amap_layout_free", "amap_layout_tensor", "amap_layout_op", "amap_layout_solve",
     "amap_layout_order", "amap_layout_copy",
+    "amap_cache_assign", "amap_rotary", "amap_cache_append", "amap_cache_attend", "amap_cache_attend_workspace",
 ]
 
 
@@ -44,7 +47,7 @@ class AmapError(RuntimeError):
     def __init__(self, status, what):
         self.status = status
         detail = ""
-        if status == AMAP_E_HIP or (status == AMAP_E_UNSUPPORTED and what.startswith(("amap_gemm", "amap_execute"))):
+        if status == AMAP_E_HIP or (status == AMAP_E_UNSUPPORTED and what.startswith(("amap_gemm", "amap_execute", "amap_cache", "amap_rotary"))):
             detail = f" [{_L.amap_last_error().decode()}]"
         super().__init__(f"{what}: {_status_str(status)} (status {status}){detail}")
 
@@ -471,6 +474,62 @@ def amap_gemm_gather(a_src_ptrs, a_map, w_src_ptr, w_map, n, out_map, out_ptr, s
     _check(_L.amap_gemm_gather(_ptr_array(a_src_ptrs, _reads(a_map)[0]), a_map.handle, w_src_ptr,
                                w_map.handle if w_map is not None else None, int(n),
                                out_map.handle if out_map is not None else None, out_ptr, stream), "amap_gemm_gather")
+
+
+class amap_heads(C.Structure):
+    _fields_ = [("data", _vp), ("type", C.c_int), ("heads", C.c_int), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class amap_rope(C.Structure):
+    _fields_ = [("freq", _vp), ("pairs", C.c_int), ("interleaved", C.c_int), ("n_axes", C.c_int), ("axis_pairs", C.c_int32 * AMAP_MAX_AXES)]
+
+
+class amap_cache(C.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("type", C.c_int), ("n_pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("page_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("k_scale", _vp), ("v_scale", _vp)]
+
+
+class amap_assign(C.Structure):
+    _fields_ = [("requests", C.c_int64), ("page_size", C.c_int), ("cached", _vp), ("fresh", _vp), ("free_pages", _vp), ("n_free", C.c_int64),
+                ("table", _vp), ("table_stride", C.c_int64), ("table_width", C.c_int), ("begin", _vp), ("length", _vp), ("slot", _vp),
+                ("position", _vp), ("owner", _vp), ("n_tokens", C.c_int64), ("taken", _vp)]
+
+
+_heads_p, _rope_p, _cache_p = C.POINTER(amap_heads), C.POINTER(amap_rope), C.POINTER(amap_cache)
+for _name, _types in (
+        ("amap_cache_assign", [C.POINTER(amap_assign), _vp]),
+        ("amap_rotary", [_heads_p, _heads_p, C.c_int64, C.c_int, _rope_p, _vp, C.c_int64, C.c_int, _vp]),
+        ("amap_cache_append", [_cache_p, _heads_p, _heads_p, C.c_int64, _vp, _rope_p, _vp, C.c_int64, _heads_p, _heads_p, _vp]),
+        ("amap_cache_attend", [_cache_p, _heads_p, C.c_int64, _vp, C.c_int64, C.c_int, _vp, C.c_float, C.c_int, _heads_p, _vp, _vp, C.c_int64, _vp]),
+        ("amap_cache_attend_workspace", [_cache_p, C.c_int, C.c_int64, C.c_int, _i64p])):
+    if hasattr(_L, _name):   # (a build of the host logic alone has none of these)
+        getattr(_L, _name).argtypes = _types
+
+
+# (structures as above; addresses and streams are integers or None)
+
+def amap_cache_assign(assign, stream=0):
+    _check(_L.amap_cache_assign(assign, _addr(stream)), "amap_cache_assign")
+
+
+def amap_rotary(x, out, tokens, head_dim, rope, position_ptr, axis_stride, inverse=False, stream=0):
+    _check(_L.amap_rotary(x, out, int(tokens), int(head_dim), rope, _addr(position_ptr), int(axis_stride), int(bool(inverse)), _addr(stream)), "amap_rotary")
+
+
+def amap_cache_append(cache, k, v, tokens, slot_ptr, rope=None, position_ptr=None, axis_stride=0, q=None, q_out=None, stream=0):
+    _check(_L.amap_cache_append(cache, k, v, int(tokens), _addr(slot_ptr), rope, _addr(position_ptr), int(axis_stride), q, q_out, _addr(stream)),
+           "amap_cache_append")
+
+
+def amap_cache_attend_workspace(cache, heads, requests, table_width):
+    n = C.c_int64()
+    _check(_L.amap_cache_attend_workspace(cache, int(heads), int(requests), int(table_width), C.byref(n)), "amap_cache_attend_workspace")
+    return n.value
+
+
+def amap_cache_attend(cache, q, requests, table_ptr, table_stride, table_width, length_ptr, scale, window, out, lse_ptr, workspace_ptr, workspace_bytes, stream=0):
+    _check(_L.amap_cache_attend(cache, q, int(requests), _addr(table_ptr), int(table_stride), int(table_width), _addr(length_ptr), float(scale), int(window),
+                                out, _addr(lse_ptr), _addr(workspace_ptr), int(workspace_bytes), _addr(stream)), "amap_cache_attend")
 
 
 class GraphDME:

@@ -15,7 +15,7 @@ LIB = os.path.join(_HERE, "libamap.so")
 CALL = os.path.join(_HERE, "_amap_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 SOURCES = ["amap_compose.cpp", "amap_graph.cpp", "amap_layout.cpp", "amap_host.cpp", "amap_plan.cpp", "amap_plan_check.cpp", "amap_kernels.hip",
-           "amap_gemm.hip", "amap_gemm_ring.hip"]
+           "amap_gemm.hip", "amap_gemm_ring.hip", "amap_cache.hip", "amap_rotary.hip", "amap_attend.hip"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",

@@ -1,0 +1,424 @@
+// Rotary positions (amap_rotary) and the store of fresh keys and values through a slot map (amap_cache_append): rows of heads
+// read once, turned where there is something to turn, rounded once and written once.
+//
+// A workgroup takes a few tokens.  It first makes their angles, one pair per lane, in LDS, where every head finds them: the
+// angle is position x frequency in 64 bits, brought into one turn there (at position 100 000 a 32-bit product is off by 4e-3
+// of a radian), its sine and cosine in 32.  Then it goes over its units, the widest piece that the rows' layout allows
+// of one head of one tensor: both halves of the pairs, or a piece that holds whole pairs, or one that is only carried
+// over.  Bound by the bytes of the rows; the angles are a 64-bit multiplication or two per pair and token, for all heads.
+#include "amap_cache.hpp"
+
+using namespace amap_cache_detail;
+using namespace amap_detail;
+using namespace amap_dev;
+
+namespace {
+
+constexpr int kTurnThreads = 256, kMaxJobs = 3, kUnitsAtOnce = 4;
+constexpr uint32_t kAnglesAtOnce = 2048;   // 16 KB of them
+constexpr int kMaxDim = 2048;
+
+// one tensor's way: where it comes from, where it goes
+struct TurnJob {
+    const char *src;
+    char *dst;
+    const float *scale;        // divide by scale[head] first (E4M3)
+    int64_t src_token, src_head, dst_token, dst_head, dst_page;   // strides in elements; dst_token: of a cache's rows
+    uint32_t units;            // of one token, heads * per_head
+    uint32_t per_head;
+    FastDiv by_head;
+    uint32_t turns, to_cache, out_type;
+};
+struct TurnArgs {
+    TurnJob job[kMaxJobs];
+    const float *freq;
+    const int32_t *position;
+    const int64_t *slot;
+    int64_t axis_stride, n_slots;
+    uint32_t tokens, dim, pairs, interleaved, n_jobs, inverse;
+    uint32_t axis_end[AMAP_MAX_AXES];
+    uint32_t page;
+    uint32_t group, splits;    // tokens of a workgroup; workgroups that share them
+    uint32_t units;            // of one token, all jobs
+    FastDiv by_token, by_split, by_pairs;
+};
+
+template <int BYTES>
+struct Piece;
+template <>
+struct Piece<16> {
+    typedef u32x4 type;
+};
+template <>
+struct Piece<8> {
+    typedef u32x2 type;
+};
+template <>
+struct Piece<4> {
+    typedef uint32_t type;
+};
+template <>
+struct Piece<2> {
+    typedef uint16_t type;
+};
+template <>
+struct Piece<1> {
+    typedef uint8_t type;
+};
+
+template <class T>
+__device__ __forceinline__ float widen(const char *at);
+template <>
+__device__ __forceinline__ float widen<F32>(const char *at) {
+    float x;
+    __builtin_memcpy(&x, at, 4);
+    return x;
+}
+template <>
+__device__ __forceinline__ float widen<Bf16>(const char *at) {
+    uint16_t x;
+    __builtin_memcpy(&x, at, 2);
+    return __uint_as_float((uint32_t)x << 16);
+}
+template <>
+__device__ __forceinline__ float widen<F16>(const char *at) {
+    _Float16 x;
+    __builtin_memcpy(&x, at, 2);
+    return (float)x;
+}
+
+// V values rounded to nearest even and stored in one access
+template <int V>
+__device__ __forceinline__ void store_as(uint32_t type, char *at, const float (&x)[V]) {
+    if (type == AMAP_F32) {
+        if constexpr (V * 4 <= 16) {
+            typename Piece<V * 4>::type p;
+            __builtin_memcpy(&p, x, sizeof(p));
+            *reinterpret_cast<typename Piece<V * 4>::type *>(at) = p;
+        }
+    } else if (type == AMAP_E4M3) {
+        uint8_t b[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float y = x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.f), 448.f);
+            b[i] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
+        }
+        typename Piece<V>::type p;
+        __builtin_memcpy(&p, b, V);
+        *reinterpret_cast<typename Piece<V>::type *>(at) = p;
+    } else {
+        uint16_t h[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            h[i] = type == AMAP_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)x[i]) : __builtin_bit_cast(uint16_t, (_Float16)x[i]);
+        typename Piece<V * 2>::type p;
+        __builtin_memcpy(&p, h, sizeof(p));
+        *reinterpret_cast<typename Piece<V * 2>::type *>(at) = p;
+    }
+}
+
+// T: the rows' type; BYTES: of one access to them
+template <class T, int BYTES>
+__global__ __launch_bounds__(kTurnThreads) void amap_turn_kernel(const TurnArgs a) {
+    constexpr int V = BYTES / T::bytes;
+    typedef typename Piece<BYTES>::type piece;
+    extern __shared__ char lds[];
+    float2 *const angle = reinterpret_cast<float2 *>(lds);   // [group][pairs]: cosine, sine
+    const uint32_t tid = threadIdx.x;
+    const uint32_t block = fdiv(blockIdx.x, a.by_split), split = blockIdx.x - block * a.splits;
+    const uint32_t t0 = block * a.group, count = min(a.group, a.tokens - t0);
+    for (uint32_t i = tid; i < count * a.pairs; i += kTurnThreads) {
+        const uint32_t t = fdiv(i, a.by_pairs), p = i - t * a.pairs;
+        uint32_t axis = 0;
+#pragma unroll
+        for (int k = 0; k + 1 < AMAP_MAX_AXES; ++k) axis += p >= a.axis_end[k];
+        const double turns = (double)a.position[axis * a.axis_stride + t0 + t] * (double)a.freq[p] * 0.15915494309189533577;   // 1 / (2 pi)
+        float s, c;
+        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+        angle[i] = make_float2(c, a.inverse ? -s : s);
+    }
+    if (a.pairs) __syncthreads();
+    const uint32_t total = count * a.units;
+    for (uint32_t base = split * kTurnThreads * kUnitsAtOnce; base < total; base += a.splits * kTurnThreads * kUnitsAtOnce) {
+        piece x[kUnitsAtOnce], y[kUnitsAtOnce];
+        char *dst[kUnitsAtOnce];
+        uint32_t at[kUnitsAtOnce], turned[kUnitsAtOnce], type[kUnitsAtOnce];   // turned: 0 carried over, 1 halves, 2 neighbours
+        float scale[kUnitsAtOnce];
+        uint32_t tok[kUnitsAtOnce];
+#pragma unroll
+        for (int k = 0; k < kUnitsAtOnce; ++k) {
+            const uint32_t i = base + k * kTurnThreads + tid;
+            dst[k] = nullptr;
+            if (i >= total) continue;
+            const uint32_t t = fdiv(i, a.by_token);
+            uint32_t u = i - t * a.units, j = 0;
+            while (j + 1 < a.n_jobs && u >= a.job[j].units) u -= a.job[j++].units;
+            const TurnJob &job = a.job[j];
+            const uint32_t head = fdiv(u, job.by_head);
+            u -= head * job.per_head;
+            const uint32_t halves = job.turns && !a.interleaved ? a.pairs / V : 0u;
+            // the unit's first element: of the first halves, then of what lies behind both
+            at[k] = u < halves ? u * V : (u + halves) * V;
+            turned[k] = u < halves ? 1u : job.turns && a.interleaved && at[k] < 2u * a.pairs ? 2u : 0u;
+            tok[k] = t;
+            type[k] = job.out_type;
+            scale[k] = job.scale ? job.scale[head] : 1.f;
+            const char *src = job.src + ((int64_t)(t0 + t) * job.src_token + (int64_t)head * job.src_head + at[k]) * T::bytes;
+            int64_t to = (int64_t)head * job.dst_head + at[k];
+            if (job.to_cache) {
+                const int64_t slot = a.slot[t0 + t];
+                if (slot < 0 || slot >= a.n_slots) continue;
+                const int64_t page = slot / a.page;
+                to += page * job.dst_page + (slot - page * a.page) * job.dst_token;
+            } else {
+                to += (int64_t)(t0 + t) * job.dst_token;
+            }
+            x[k] = *reinterpret_cast<const piece *>(src);
+            if (turned[k] == 1u) y[k] = *reinterpret_cast<const piece *>(src + (size_t)a.pairs * T::bytes);
+            const uint32_t es = type[k] == AMAP_F32 ? 4u : type[k] == AMAP_E4M3 ? 1u : 2u;
+            dst[k] = job.dst + to * es;
+        }
+#pragma unroll
+        for (int k = 0; k < kUnitsAtOnce; ++k) {
+            if (!dst[k]) continue;
+            float u[V], w[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) u[v] = widen<T>(reinterpret_cast<const char *>(&x[k]) + v * T::bytes);
+            const float2 *const cs = angle + tok[k] * a.pairs;
+            if (turned[k] == 1u) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float b = widen<T>(reinterpret_cast<const char *>(&y[k]) + v * T::bytes), f = u[v];
+                    const float2 t = cs[at[k] + v];
+                    u[v] = f * t.x - b * t.y;
+                    w[v] = b * t.x + f * t.y;
+                }
+                if (scale[k] != 1.f) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) w[v] /= scale[k];
+                }
+                const uint32_t es = type[k] == AMAP_F32 ? 4u : type[k] == AMAP_E4M3 ? 1u : 2u;
+                store_as<V>(type[k], dst[k] + a.pairs * es, w);
+            } else if (turned[k] == 2u) {
+                if constexpr (V > 1) {
+#pragma unroll
+                    for (int v = 0; v < V; v += 2)
+                        if (at[k] + v < 2u * a.pairs) {
+                            const float f = u[v], b = u[v + 1];
+                            const float2 t = cs[(at[k] + v) >> 1];
+                            u[v] = f * t.x - b * t.y;
+                            u[v + 1] = b * t.x + f * t.y;
+                        }
+                }
+            }
+            if (scale[k] != 1.f) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) u[v] /= scale[k];
+            }
+            store_as<V>(type[k], dst[k], u);
+        }
+    }
+}
+
+bool rope_fits(const amap_rope *r, int dim, amap_status &st) {
+    st = AMAP_E_INVALID;
+    if (!r->freq || r->pairs < 1 || r->n_axes < 1 || r->n_axes > AMAP_MAX_AXES) return false;
+    int64_t sum = 0;
+    for (int i = 0; i < r->n_axes; ++i) {
+        if (r->axis_pairs[i] < 0) return false;
+        sum += r->axis_pairs[i];
+    }
+    st = AMAP_E_SHAPE;
+    return sum == r->pairs && r->pairs <= dim / 2;
+}
+
+// The widest access that all rows of the jobs allow, 16 bytes of the rows' type at most, down to one element (two of them where neighbours are
+// pairs: whole pairs in a unit).
+struct Way {
+    const amap_heads *in;
+    void *dst;
+    amap_type out;
+    int64_t token, head, page;   // of dst
+    bool turns, to_cache;
+    const float *scale;
+};
+
+template <class T, int BYTES>
+hipError_t turn(const TurnArgs &g, uint32_t grid, uint32_t lds, hipStream_t s) {
+    return launch_kernel<amap_turn_kernel<T, BYTES>>(dim3(grid), dim3(kTurnThreads), lds, s, g);
+}
+template <class T>
+hipError_t turn_by(int bytes, const TurnArgs &g, uint32_t grid, uint32_t lds, hipStream_t s) {
+    if (bytes == 16) return turn<T, 16>(g, grid, lds, s);
+    if (bytes == 8) return turn<T, 8>(g, grid, lds, s);
+    if (T::bytes == 2 && bytes == 2) return turn<T, T::bytes>(g, grid, lds, s);
+    return turn<T, 4>(g, grid, lds, s);
+}
+
+amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope *rope, const int32_t *position, int64_t axis_stride, int inverse, const int64_t *slot,
+                const amap_cache *cache, hipStream_t s) {
+    const amap_type type = way[0].in->type;
+    const int es = bytes_of(type);
+    // ---- the width: what divides every offset, in elements, and in bytes on both sides
+    uint64_t elements = (uint64_t)dim;
+    uint64_t most = 16 / es;
+    if (rope) elements |= rope->interleaved ? 0u : (uint64_t)rope->pairs;
+    for (int i = 0; i < n; ++i) {
+        const Way &w = way[i];
+        const uint64_t out = (uint64_t)bytes_of(w.out);
+        if (tokens > 1) elements |= (uint64_t)w.in->token_stride;
+        if (w.in->heads > 1) elements |= (uint64_t)w.in->head_stride | (uint64_t)w.head;
+        elements |= w.to_cache ? (uint64_t)w.token | (uint64_t)w.page : tokens > 1 ? (uint64_t)w.token : 0u;
+        const uint64_t in_at = reinterpret_cast<uintptr_t>(w.in->data), out_at = reinterpret_cast<uintptr_t>(w.dst);
+        if (in_at % es || out_at % out) return refuse("a tensor that does not begin at a whole element");
+        elements |= in_at / es | out_at / out;
+        most = most < 16 / out ? most : 16 / out;
+    }
+    uint64_t width = aligned_to(elements, most);
+    if (rope && rope->interleaved && width < 2) {   // pairs of two elements in one access, where rows allow no wider one: an odd element
+        return refuse("neighbouring pairs need rows that begin at even elements, and an even head_dim");
+    }
+    TurnArgs g = {};
+    g.n_jobs = (uint32_t)n;
+    g.tokens = (uint32_t)tokens;
+    g.dim = (uint32_t)dim;
+    if (rope) {
+        g.freq = rope->freq;
+        g.position = position;
+        g.axis_stride = axis_stride;
+        g.pairs = (uint32_t)rope->pairs;
+        g.interleaved = rope->interleaved != 0;
+        g.inverse = inverse != 0;
+        uint32_t end = 0;
+        for (int i = 0; i < AMAP_MAX_AXES; ++i) {
+            if (i < rope->n_axes) end += (uint32_t)rope->axis_pairs[i];
+            g.axis_end[i] = i + 1 < rope->n_axes ? end : 0xFFFFFFFFu;   // (the last axis has the rest)
+        }
+    }
+    if (cache) {
+        g.slot = slot;
+        g.n_slots = cache->n_pages * cache->page_size;
+        g.page = (uint32_t)cache->page_size;
+    }
+    const uint32_t per_head = (uint32_t)(dim / (int)width), halves = rope && !rope->interleaved ? (uint32_t)rope->pairs / (uint32_t)width : 0u;
+    uint64_t units = 0;
+    for (int i = 0; i < n; ++i) {
+        const Way &w = way[i];
+        TurnJob &j = g.job[i];
+        j.src = static_cast<const char *>(w.in->data);
+        j.dst = static_cast<char *>(w.dst);
+        j.scale = w.scale;
+        j.src_token = w.in->token_stride;
+        j.src_head = w.in->head_stride;
+        j.dst_token = w.token;
+        j.dst_head = w.head;
+        j.dst_page = w.page;
+        j.per_head = w.turns ? per_head - halves : per_head;
+        j.units = j.per_head * (uint32_t)w.in->heads;
+        j.by_head = make_fastdiv(j.per_head);
+        j.turns = w.turns;
+        j.to_cache = w.to_cache;
+        j.out_type = w.out;
+        units += j.units;
+    }
+    if (units > (1u << 24)) return refuse("more than 2^24 pieces in the rows of one token");
+    g.units = (uint32_t)units;
+    g.by_token = make_fastdiv(g.units);
+    g.by_pairs = make_fastdiv(g.pairs ? g.pairs : 1u);
+    // tokens of a workgroup: two passes over its units, as far as their angles find room
+    const uint32_t pass = kTurnThreads * kUnitsAtOnce;
+    uint64_t group = 2 * pass / units;
+    if (g.pairs && group > kAnglesAtOnce / g.pairs) group = kAnglesAtOnce / g.pairs;
+    if (group < 1) group = 1;
+    // few tokens: fewer of them each, down to one, and several workgroups to one token
+    while (group > 1 && (uint64_t)tokens < 512 * group) group = (group + 1) / 2;
+    const uint64_t blocks = ((uint64_t)tokens + group - 1) / group, passes = (group * units + pass - 1) / pass;
+    uint64_t splits = blocks >= 512 ? 1 : passes;
+    if (blocks * splits >= (1u << 31)) return refuse("too many tokens for one launch");
+    g.group = (uint32_t)group;
+    g.splits = (uint32_t)splits;
+    g.by_split = make_fastdiv(g.splits);
+    const uint32_t lds = g.group * g.pairs * 8u, grid = (uint32_t)(blocks * splits);
+    const StreamDevice device(s);
+    if (device.status() != hipSuccess) return launched(device.status(), "the stream's device");
+    const int bytes = (int)width * es;
+    const hipError_t e = type == AMAP_F32    ? turn_by<F32>(bytes, g, grid, lds, s)
+                         : type == AMAP_BF16 ? turn_by<Bf16>(bytes, g, grid, lds, s)
+                                             : turn_by<F16>(bytes, g, grid, lds, s);
+    return launched(e, "amap_turn_kernel");
+}
+
+// a tensor of rows that a call reads or writes
+amap_status check_rows(const amap_heads *h, int64_t tokens, int dim, bool written, Box &box) {
+    if (!h || !h->data || h->heads < 1 || !is_wide(h->type)) return AMAP_E_INVALID;
+    box = box_of(*h, tokens, dim);
+    return box.fits && (!written || box.apart) ? AMAP_OK : AMAP_E_SHAPE;
+}
+
+bool same_rows(const amap_heads &a, const amap_heads &b) { return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride; }
+
+amap_status check_turn(const amap_heads *x, const amap_heads *out, int64_t tokens, int dim, Box &from, Box &to) {
+    amap_status st = check_rows(x, tokens, dim, false, from);
+    if (st == AMAP_OK) st = check_rows(out, tokens, dim, true, to);
+    if (st != AMAP_OK) return st;
+    if (x->type != out->type) return AMAP_E_INVALID;
+    if (x->heads != out->heads) return AMAP_E_SHAPE;
+    return meet(from, to) && !same_rows(*x, *out) ? AMAP_E_ALIAS : AMAP_OK;
+}
+
+amap_status check_sizes(int64_t tokens, int dim) {
+    if (tokens < 0 || dim < 1) return AMAP_E_INVALID;
+    if (tokens > INT32_MAX) return AMAP_E_SHAPE;
+    return dim > kMaxDim ? refuse("heads of more than 2048 elements") : AMAP_OK;
+}
+
+}  // namespace
+
+extern "C" amap_status amap_rotary(const amap_heads *x, const amap_heads *out, int64_t tokens, int head_dim, const amap_rope *rope, const int32_t *position,
+                                   int64_t axis_stride, int inverse, void *stream) {
+    if (!x || !out || !rope) return AMAP_E_INVALID;
+    amap_status st = check_sizes(tokens, head_dim);
+    if (st != AMAP_OK) return st;
+    if (!rope_fits(rope, head_dim, st)) return st;
+    if (tokens == 0) return AMAP_OK;
+    if (!position || axis_stride < 0) return AMAP_E_INVALID;
+    Box from, to;
+    st = check_turn(x, out, tokens, head_dim, from, to);
+    if (st != AMAP_OK) return st;
+    const Way way{x, out->data, out->type, out->token_stride, out->head_stride, 0, true, false, nullptr};
+    return run(&way, 1, tokens, head_dim, rope, position, axis_stride, inverse, nullptr, nullptr, reinterpret_cast<hipStream_t>(stream));
+}
+
+extern "C" amap_status amap_cache_append(const amap_cache *cache, const amap_heads *k, const amap_heads *v, int64_t tokens, const int64_t *slot, const amap_rope *rope,
+                                         const int32_t *position, int64_t axis_stride, const amap_heads *q, const amap_heads *q_out, void *stream) {
+    Box ck, cv, rows[3], to;
+    amap_status st = check_cache(cache, ck, cv);
+    if (st != AMAP_OK) return st;
+    const int dim = cache->head_dim;
+    if (!k || !v || (q != nullptr) != (q_out != nullptr) || (q && !rope)) return AMAP_E_INVALID;
+    st = check_sizes(tokens, dim);
+    if (st != AMAP_OK) return st;
+    if (rope && !rope_fits(rope, dim, st)) return st;
+    if (tokens == 0) return AMAP_OK;
+    if (!slot || (rope && (!position || axis_stride < 0))) return AMAP_E_INVALID;
+    st = check_rows(k, tokens, dim, false, rows[0]);
+    if (st == AMAP_OK) st = check_rows(v, tokens, dim, false, rows[1]);
+    if (st != AMAP_OK) return st;
+    if (k->type != v->type || (q && q->type != k->type)) return AMAP_E_INVALID;
+    if (k->heads != cache->kv_heads || v->heads != cache->kv_heads) return AMAP_E_SHAPE;
+    int n = 2;
+    Way way[kMaxJobs] = {{k, cache->k, cache->type, cache->token_stride, cache->head_stride, cache->page_stride, rope != nullptr, true, cache->k_scale},
+                         {v, cache->v, cache->type, cache->token_stride, cache->head_stride, cache->page_stride, false, true, cache->v_scale},
+                         {}};
+    if (q) {
+        st = check_turn(q, q_out, tokens, dim, rows[2], to);
+        if (st != AMAP_OK) return st;
+        if (meet(to, ck) || meet(to, cv)) return AMAP_E_ALIAS;
+        // (q may lie between k and v in one projection, and be turned there in place)
+        if (!same_rows(*q, *q_out) && (meet(to, rows[0]) || meet(to, rows[1]))) return AMAP_E_ALIAS;
+        way[n++] = Way{q, q_out->data, q_out->type, q_out->token_stride, q_out->head_stride, 0, true, false, nullptr};
+    }
+    for (int i = 0; i < n; ++i)
+        if (meet(rows[i], ck) || meet(rows[i], cv)) return AMAP_E_ALIAS;
+    return run(way, n, tokens, dim, rope, position, axis_stride, 0, slot, cache, reinterpret_cast<hipStream_t>(stream));
+}

@@ -2,6 +2,9 @@
 libamap.so; nothing here computes, and there is no CPU fallback."""
 from __future__ import annotations
 
+import contextlib
+from typing import NamedTuple
+
 import numpy as np
 import torch
 
@@ -101,3 +104,206 @@ def gemm_fused(a_src: torch.Tensor, a_map, w: torch.Tensor, out=None, stream=Non
     else:
         B.amap_gemm_fused_store(a_src.data_ptr(), a_map, w.data_ptr(), n, out_map, out.data_ptr(), st)
     return out
+
+
+# ---- a paged key-value cache: block tables and slots, rotary positions, the store of fresh tokens, one token's attention
+
+# (a tensor of 16-bit words holds bf16 bits, as everywhere in this package)
+_ELEMENT = {torch.float32: B.AMAP_F32, torch.bfloat16: B.AMAP_BF16, torch.int16: B.AMAP_BF16, torch.float16: B.AMAP_F16, torch.float8_e4m3fn: B.AMAP_E4M3}
+
+
+def _refused(what, why, status=B.AMAP_E_INVALID):
+    return B.AmapError(status, f"{what}: {why}")
+
+
+def _on_gpu(t, dtype, rank, what, name):
+    """The tensor, on a GPU, of this type and rank, its last dimension contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.dim() != rank:
+        raise _refused(what, f"{name} is no {dtype} tensor of {rank} dimension{'s' * (rank > 1)}")
+    if not t.is_cuda:
+        raise _refused(what, f"{name} is not on the GPU")
+    if rank and t.size(-1) > 1 and t.stride(-1) != 1:
+        raise _refused(what, f"{name} is not contiguous along its last dimension", B.AMAP_E_UNSUPPORTED)
+    return t
+
+
+def _rows(t, what, name):
+    """A [tokens, heads, head_dim] tensor as the library takes it."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _ELEMENT:
+        raise _refused(what, f"{name} is no tensor of a known type")
+    _on_gpu(t, t.dtype, 3, what, name)
+    return B.amap_heads(t.data_ptr(), _ELEMENT[t.dtype], t.size(1), t.stride(0), t.stride(1))
+
+
+class Rope:
+    """Rotary positions: freq [pairs] (float32, on the GPU), the pairs of each axis, and which elements make a pair: (p, p + pairs), or
+    (2p, 2p + 1) if interleaved."""
+
+    def __init__(self, freq, axis_pairs=None, interleaved=False):
+        self.freq = _on_gpu(freq, torch.float32, 1, "Rope", "freq")
+        self.axis_pairs = (freq.numel(),) if axis_pairs is None else tuple(int(n) for n in axis_pairs)
+        self.interleaved = bool(interleaved)
+        if not 1 <= len(self.axis_pairs) <= B.AMAP_MAX_AXES or min(self.axis_pairs) < 0 or sum(self.axis_pairs) != freq.numel():
+            raise _refused("Rope", f"axis_pairs {self.axis_pairs} are not the {freq.numel()} pairs", B.AMAP_E_SHAPE)
+        self._c = B.amap_rope(freq.data_ptr(), freq.numel(), int(self.interleaved), len(self.axis_pairs), (B.C.c_int32 * B.AMAP_MAX_AXES)(*self.axis_pairs))
+
+    def _positions(self, position, tokens, what):
+        """The address of [axes, tokens] or [tokens] int32 positions (the latter the same for all axes), and the step between axes."""
+        if position is None:
+            raise _refused(what, "a rope without positions")
+        if isinstance(position, torch.Tensor) and position.dim() == 2:
+            _on_gpu(position, torch.int32, 2, what, "position")
+            if position.size(0) != len(self.axis_pairs) or position.size(1) != tokens:
+                raise _refused(what, f"position is {tuple(position.shape)}, not {(len(self.axis_pairs), tokens)}", B.AMAP_E_SHAPE)
+            return position.data_ptr(), position.stride(0)
+        _on_gpu(position, torch.int32, 1, what, "position")
+        if position.size(0) != tokens:
+            raise _refused(what, f"position is {tuple(position.shape)}, not {(tokens,)}", B.AMAP_E_SHAPE)
+        return position.data_ptr(), 0
+
+
+class PagedCache:
+    """Keys and values as [pages, page_size, kv_heads, head_dim] tensors of one type and one set of strides: any memory order with
+    the elements of a head side by side (a heads-first cache is the permuted view of one).  float8_e4m3fn with a
+    float32 scale per head, or none."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        for t, name in ((k, "k"), (v, "v")):
+            if not isinstance(t, torch.Tensor) or _ELEMENT.get(t.dtype, B.AMAP_F32) == B.AMAP_F32:
+                raise _refused("PagedCache", f"{name} is no tensor of a cache's type")
+            _on_gpu(t, t.dtype, 4, "PagedCache", name)
+        if k.dtype != v.dtype or k.shape != v.shape or k.stride() != v.stride():
+            raise _refused("PagedCache", "k and v differ in type, shape or strides", B.AMAP_E_SHAPE)
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t is not None and (_on_gpu(t, torch.float32, 1, "PagedCache", name).numel() != k.size(2) or k.dtype != torch.float8_e4m3fn):
+                raise _refused("PagedCache", f"{name} is one scale per head of an 8-bit cache", B.AMAP_E_SHAPE)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._c = B.amap_cache(k.data_ptr(), v.data_ptr(), _ELEMENT[k.dtype], k.size(0), k.size(1), k.size(2), k.size(3), k.stride(0), k.stride(1), k.stride(2),
+                               None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
+
+    @property
+    def page_size(self):
+        return self.k.size(1)
+
+
+class Assigned(NamedTuple):
+    begin: torch.Tensor      # [requests + 1] int32: where each request's fresh tokens begin
+    length: torch.Tensor     # [requests] int32: tokens after the step
+    slot: torch.Tensor       # [n_tokens] int64: page * page_size + row, -1 where there is none
+    position: torch.Tensor   # [n_tokens] int32
+    owner: torch.Tensor      # [n_tokens] int32: the request
+    taken: torch.Tensor      # [1] int32: pages needed from the list
+
+
+def assigned_buffers(requests, n_tokens, like=None) -> Assigned:
+    """Room for a step's assignment, for a program that keeps it from step to step (as a captured graph has to)."""
+    dev = require_gpu() if like is None else like.device
+    i32 = torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=dev)
+    slot = torch.empty(n_tokens, dtype=torch.int64, device=dev)
+    begin, length, taken, position, owner = torch.split(i32, (requests + 1, requests, 1, n_tokens, n_tokens))
+    return Assigned(begin, length, slot, position, owner, taken)
+
+
+def _made_on(stream):
+    """Where a tensor has to be made that `stream` is the first to use: memory of the current stream may still be in use there, and
+    what is given back to it may be handed out before `stream` is done."""
+    if stream is None or stream == current_stream():
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream())
+
+
+def cache_assign(page_size, cached, fresh, table, free_pages, n_tokens, out=None, stream=None) -> Assigned:
+    """Pages, slots and positions for a step in which request r adds fresh[r] tokens to its cached[r] (None: none yet):
+    new pages are taken from the head of free_pages into `table`, which is changed in place.  All int32."""
+    what = "amap_cache_assign"
+    n = _on_gpu(fresh, torch.int32, 1, what, "fresh").size(0)
+    _on_gpu(table, torch.int32, 2, what, "table")
+    _on_gpu(free_pages, torch.int32, 1, what, "free_pages")
+    if cached is not None and _on_gpu(cached, torch.int32, 1, what, "cached").size(0) != n or table.size(0) != n:
+        raise _refused(what, "cached, fresh and table are not of the same requests", B.AMAP_E_SHAPE)
+    if out is None:
+        with _made_on(stream):
+            out = assigned_buffers(n, n_tokens, fresh)
+    else:
+        sizes = (n + 1, n, n_tokens, n_tokens, n_tokens, 1)
+        for t, size, dtype, name in zip(out, sizes, (torch.int32, torch.int32, torch.int64, torch.int32, torch.int32, torch.int32), Assigned._fields):
+            if _on_gpu(t, dtype, 1, what, name).size(0) != size:
+                raise _refused(what, f"{name} holds {t.size(0)} entries, not {size}", B.AMAP_E_SHAPE)
+    B.amap_cache_assign(B.amap_assign(n, page_size, None if cached is None else cached.data_ptr(), fresh.data_ptr(), free_pages.data_ptr(), free_pages.size(0),
+                                      table.data_ptr(), table.stride(0), table.size(1), out.begin.data_ptr(), out.length.data_ptr(), out.slot.data_ptr(),
+                                      out.position.data_ptr(), out.owner.data_ptr(), n_tokens, out.taken.data_ptr()),
+                        current_stream() if stream is None else stream)
+    return out
+
+
+def rotary(x, rope, position, out=None, inverse=False, stream=None) -> torch.Tensor:
+    """out = x [tokens, heads, head_dim] turned to its positions ([tokens] or [axes, tokens], int32); inverse: turned back, the
+    gradient.  out may be x itself."""
+    what = "amap_rotary"
+    a = _rows(x, what, "x")
+    if out is None:
+        with _made_on(stream):
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    elif isinstance(out, torch.Tensor) and out.shape != x.shape:
+        raise _refused(what, f"out is {tuple(out.shape)}, not {tuple(x.shape)}", B.AMAP_E_SHAPE)
+    at, step = rope._positions(position, x.size(0), what)
+    B.amap_rotary(a, _rows(out, what, "out"), x.size(0), x.size(2), rope._c, at, step, inverse, current_stream() if stream is None else stream)
+    return out
+
+
+def cache_append(cache, k, v, slot, rope=None, position=None, q=None, q_out=None, stream=None):
+    """k and v [tokens, kv_heads, head_dim] into the cache at slot [tokens] (int64; outside the cache: left out), k turned by the
+    rope on the way, if there is one, and q into q_out (allocated if None; returned)."""
+    what = "amap_cache_append"
+    a, b = _rows(k, what, "k"), _rows(v, what, "v")
+    tokens, dim = k.size(0), cache.k.size(3)
+    if v.size(0) != tokens or k.size(2) != dim or v.size(2) != dim or (q is not None and isinstance(q, torch.Tensor) and (q.size(0) != tokens or q.size(-1) != dim)):
+        raise _refused(what, "k, v, q and the cache differ in tokens or head_dim", B.AMAP_E_SHAPE)
+    if _on_gpu(slot, torch.int64, 1, what, "slot").size(0) != tokens:
+        raise _refused(what, f"slot holds {slot.size(0)} entries, not {tokens}", B.AMAP_E_SHAPE)
+    at, step = (None, 0) if rope is None else rope._positions(position, tokens, what)
+    c = d = None
+    if q is not None:
+        c = _rows(q, what, "q")
+        if q_out is None:
+            with _made_on(stream):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif isinstance(q_out, torch.Tensor) and q_out.shape != q.shape:
+            raise _refused(what, f"q_out is {tuple(q_out.shape)}, not {tuple(q.shape)}", B.AMAP_E_SHAPE)
+        d = _rows(q_out, what, "q_out")
+    B.amap_cache_append(cache._c, a, b, tokens, slot.data_ptr(), None if rope is None else rope._c, at, step, c, d, current_stream() if stream is None else stream)
+    return q_out
+
+
+def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=None, workspace=None, stream=None):
+    """(out, lse): the attention of q [requests, heads, head_dim] over the first length[r] tokens (int32; window > 0: the last
+    `window` of them) that table [requests, width] (int32) leads to.  scale: 1 / sqrt(head_dim) if None.  A request that sees nothing has
+    rows of 0 and lse -inf.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it."""
+    what = "amap_cache_attend"
+    a = _rows(q, what, "q")
+    n, heads, dim = q.shape
+    _on_gpu(table, torch.int32, 2, what, "table")
+    if _on_gpu(length, torch.int32, 1, what, "length").size(0) != n or table.size(0) != n or dim != cache.k.size(3):
+        raise _refused(what, "q, table, length and the cache differ in requests or head_dim", B.AMAP_E_SHAPE)
+    need = B.amap_cache_attend_workspace(cache._c, heads, n, table.size(1))
+    with _made_on(stream):
+        if out is None:
+            out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if isinstance(out, torch.Tensor) and out.shape != q.shape:
+        raise _refused(what, f"out is {tuple(out.shape)}, not {tuple(q.shape)}", B.AMAP_E_SHAPE)
+    if _on_gpu(lse, torch.float32, 2, what, "lse").shape != (n, heads) or not lse.is_contiguous():
+        raise _refused(what, f"lse is no contiguous {(n, heads)}", B.AMAP_E_SHAPE)
+    have = 0 if workspace is None else _on_gpu(workspace, torch.uint8, 1, what, "workspace").numel()
+    B.amap_cache_attend(cache._c, a, n, table.data_ptr(), table.stride(0), table.size(1), length.data_ptr(), dim ** -0.5 if scale is None else scale, window,
+                        _rows(out, what, "out"), lse.data_ptr(), None if workspace is None else workspace.data_ptr(), have,
+                        current_stream() if stream is None else stream)
+    return out, lse
+
+
+def attend_workspace(cache, heads, requests, table_width) -> int:
+    """Bytes of workspace that cache_attend takes for such a call."""
+    return B.amap_cache_attend_workspace(cache._c, heads, requests, table_width)
