@@ -3,11 +3,11 @@
 //
 // Bound by the cache's bytes: every visible key and value is read once, and 2 heads / kv_heads flop are done with each byte.  So the
 // kernel is built around keeping loads in flight.
-//   Work: tiles of 32 tokens for each wavefront of a workgroup.  The tiles of all requests and key heads are one line, cut into equal
+//   Work: tiles of 32 tokens, a workgroup is one wavefront.  The tiles of all requests and key heads are one line, cut into equal
 //     shares, one for each workgroup of a grid that fills the chip once: long requests are split, short ones follow one
 //     another, whatever the mix, and only where a cut falls inside a request are results joined (amap_attend_join_kernel).
-//   Loads: keys, values and the table's entries go straight into LDS (global_load_lds), a ring of stages per wavefront, waited for by count.
-//     No wavefront waits for another before its share of a request is done.  A token that is not visible is read from 16 bytes of
+//   Loads: keys, values and the table's entries go straight into LDS (global_load_lds), a ring of two stages, waited for by count.
+//     No wavefront waits for another; while one begins or ends a request its neighbours on the compute unit keep loading.  A token that is not visible is read from 16 bytes of
 //     zeros, so nothing that lies in the cache behind a request's end comes near the sums.
 //   Products: the scores as K Q^T, 32 tokens by 16 columns (the queries that share a key head), by 16 x 16 x 32 matrix instructions.  The tokens
 //     are dealt to the rows of the two tiles so that a lane ends up with 8 consecutive ones: just what the next product,
@@ -16,6 +16,8 @@
 //     the result's own rounding is.  With up to 8 queries to a key head the second part costs nothing: it takes the columns that are
 //     idle.  (A value that is infinite makes its column NaN, as 0 * inf does in the sum itself where a weight has vanished.)
 #include "amap_cache.hpp"
+
+#include <type_traits>
 
 using namespace amap_cache_detail;
 using namespace amap_detail;
@@ -27,12 +29,15 @@ constexpr uint32_t kUnits = 256;   // compute units of an MI355X
 constexpr int kTokens = 32;        // of a wavefront's step
 constexpr int kColumns = 16;       // queries of a workgroup at a time (8 where their weights' second parts have the others)
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
+constexpr uint32_t kFewSegments = 128;     // up to so many are joined row by row: they are in many pieces each
+constexpr uint32_t kMostJoining = 4096;    // workgroups of a join
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
 struct AttendArgs {
     const char *k, *v, *q;
     char *out;
     float *lse, *parts;
+    struct Split *splits;
     const float *k_scale, *v_scale;
     const int32_t *table, *length;
     int64_t table_stride, q_token, q_head, out_token, out_head;
@@ -42,13 +47,13 @@ struct AttendArgs {
     uint32_t heads, columns, segments;           // segments of a request: kv_heads times the column blocks of one
     FastDiv by_page, by_segments, by_blocks;
     uint32_t blocks, least;                      // column blocks of a key head; tiles of a share, at least
-    uint32_t window, aligned;                    // aligned: q in whole 16-byte pieces
+    uint32_t window, aligned, halves;            // aligned: q in whole 16-byte pieces; halves: 16 tokens from a multiple of 16 on lie in one page
     float scale;
 };
 
-// What a workgroup leaves for the join: of the segment that begins in its share and goes on in the next ones.
+// Of each segment, for the join: the workgroup in whose share it begins and in how many pieces it is (0: in none, the result is there).
 struct Split {
-    uint32_t request, segment, count, pad;
+    uint32_t group, count;
 };
 
 __device__ const u32x4 kZeros = {0u, 0u, 0u, 0u};
@@ -99,18 +104,16 @@ struct Form {
     static constexpr int ES = ES_, DP = DP_;
     static constexpr bool PAIRED = PAIRED_;                 // the weights' second parts in columns 8 .. 15
     static constexpr int ROW = DP * ES, NC = ROW / 16;      // bytes and 16-byte pieces of a row in LDS
-    static constexpr int WAVES = ROW > 256 ? 2 : 4;
-    static constexpr int STAGES = ROW <= 64 ? 4 : ROW <= 96 ? 3 : 2;
+    static constexpr int STAGES = 2;
     static constexpr int SIDE = kTokens * ROW, STAGE = 2 * SIDE;
-    static constexpr int LOADS = NC / 2;                    // of a side, 1 KB each
+    static constexpr int LOADS = NC / 2;                    // of a side, 1 KB each (of the keys, and one of the table's entries)
     static constexpr int IDS = STAGES * 256;                // a word per lane and stage
-    static constexpr int PER_WAVE = STAGES * STAGE + IDS;
     static constexpr int OUT_ROW = DP + 4;                  // floats; the 4 spread a wavefront's rows over the banks
-    static constexpr int LDS = WAVES * PER_WAVE;
-    static constexpr int PER_UNIT = at_most(4, 160 * 1024 / LDS);
-    static constexpr int TILE = kTokens * WAVES;
-    static_assert(kColumns * OUT_ROW * 4 <= STAGES * STAGE && LDS <= 160 * 1024, "a wavefront's result takes the place of its stages");
-    static_assert((STAGES - 1) * (2 * LOADS + 1) + LOADS < 64, "vmcnt");
+    static constexpr int LDS = STAGES * STAGE + IDS;
+    static constexpr int PER_UNIT = at_most(16, 160 * 1024 / LDS);   // workgroups that a compute unit holds at once
+    static_assert(kColumns * OUT_ROW * 4 <= STAGES * STAGE && LDS <= 160 * 1024, "the results take the place of the stages");
+    static constexpr bool HALVES = NC % 4 == 0;             // whether a load's rows are of one half of the tile
+    static_assert(3 * LOADS + 2 < 64, "vmcnt");
 };
 
 // ---- where things lie in a stage: rows of NC pieces, a piece's place XOR-ed with bits of its row, so that what one LDS access serves together (16
@@ -146,17 +149,38 @@ __device__ __forceinline__ void landed() {
     static_assert(N < 64, "vmcnt");
     asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
 }
-// all but the newest `later` batches of L loads have landed
-template <int L, int R>
-__device__ __forceinline__ void landed_but(uint32_t later) {
-    if constexpr (R == 0) {
-        landed<0>();
-    } else {
-        if (later >= (uint32_t)R)
-            landed<R * L>();
+// N loads of 16 bytes a lane, 1 KB apart in LDS: load i from base + off[i] (off counts 4096 - 1024 (i % 4) on top: the instruction's offset counts on both
+// sides, so that one write of M0 serves four; base is 4096 less).  The first half of them from `lo`, the others from `hi`.
+template <int N>
+__device__ __forceinline__ void load_rows(const char *lo, const char *hi, const uint32_t (&off)[N], uint32_t lds) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const uint32_t at = lds + 1024u * i;
+        const char *const b0 = 2 * i < N ? lo : hi, *const b1 = 2 * i + 2 < N ? lo : hi, *const b2 = 2 * i + 4 < N ? lo : hi, *const b3 = 2 * i + 6 < N ? lo : hi;
+        if (i + 4 <= N)
+            asm volatile(
+                "s_mov_b32 m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %5 offset:1024\n\t"
+                "global_load_lds_dwordx4 %2, %6 offset:2048\n\tglobal_load_lds_dwordx4 %3, %7 offset:3072" ::"v"(off[i]),
+                "v"(off[i + 1 < N ? i + 1 : 0]), "v"(off[i + 2 < N ? i + 2 : 0]), "v"(off[i + 3 < N ? i + 3 : 0]), "s"(b0), "s"(b1), "s"(b2), "s"(b3), "s"(at)
+                : "memory");
         else
-            landed_but<L, R - 1>(later);
+            asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024" ::"v"(off[i]),
+                         "v"(off[i + 1 < N ? i + 1 : 0]), "s"(b0), "s"(b1), "s"(at)
+                         : "memory");
     }
+}
+// the larger (sum) of what the four lanes of one column hold
+__device__ __forceinline__ float top_of_column(float x) {
+    const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
+    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+__device__ __forceinline__ float sum_of_column(float x) {
+    const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(u[0]) + __uint_as_float(u[1]);
+    const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
 }
 
 typedef __attribute__((address_space(3))) char lds_char;
@@ -173,97 +197,102 @@ __device__ __forceinline__ void lds_put(uint32_t at, X x) {
 struct Seen {
     uint32_t first, past, tile, tiles;
 };
-template <int TILE>
 __device__ __forceinline__ Seen seen_of(const AttendArgs &a, uint32_t r) {
     Seen s;
     s.past = min((uint32_t)max(a.length[r], 0), a.most);
     s.first = a.window && s.past > a.window ? s.past - a.window : 0u;
-    s.tile = s.first / TILE;
-    s.tiles = (s.past + TILE - 1) / TILE - s.tile;
+    s.tile = s.first / kTokens;
+    s.tiles = (s.past + kTokens - 1) / kTokens - s.tile;
     return s;
+}
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t x, uint32_t lane) {   // over the lanes, this one's included
+#pragma unroll
+    for (uint32_t d = 1; d < 64; d <<= 1) {
+        const uint32_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
 }
 
 template <class F>
-__global__ __launch_bounds__(64 * F::WAVES, F::PER_UNIT) void amap_attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64) void amap_attend_kernel(const AttendArgs a) {
     typedef typename Of<typename F::T>::eight eight;
-    constexpr uint32_t kThreads = 64 * F::WAVES;
     extern __shared__ char smem[];
-    __shared__ uint32_t sums[F::WAVES], found[4];
-    __shared__ float top[F::WAVES][kColumns], total[F::WAVES][kColumns];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t g = lane >> 4, col = lane & 15u;
-    const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)smem + wave * F::PER_WAVE, ids = base + F::STAGES * F::STAGE;
+    const uint32_t lane = threadIdx.x, g = lane >> 4, col = lane & 15u;
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)smem, ids = base + F::STAGES * F::STAGE;
 
-    // ---- the share: tiles of all requests, and of those before each
+    // ---- the share: tiles of all requests, an equal run of them to a lane
+    const uint32_t run = (a.requests + 63u) >> 6, r0 = min(lane * run, a.requests), r1 = min(r0 + run, a.requests);
     uint32_t tiles = 0;
-    for (uint32_t r = tid; r < a.requests; r += kThreads) tiles += seen_of<F::TILE>(a, r).tiles;
-#pragma unroll
-    for (int d = 32; d; d >>= 1) tiles += __shfl_xor(tiles, d);
-    if (lane == 0) sums[wave] = tiles;
-    __syncthreads();
-    uint32_t all = 0;
-#pragma unroll
-    for (int w = 0; w < F::WAVES; ++w) all += sums[w];
-    all *= a.segments;
+    for (uint32_t r = r0; r < r1; ++r) tiles += seen_of(a, r).tiles;
+    const uint32_t upto = sum_up_to(tiles, lane), all = __builtin_amdgcn_readlane(upto, 63) * a.segments;
     const uint32_t share = max(a.least, (all + gridDim.x - 1) / gridDim.x);
     uint32_t u = blockIdx.x * share;
     const uint32_t end = min(u + share, all);
     // rows that see nothing, request by request over the workgroups
     for (uint32_t r = blockIdx.x; r < a.requests; r += gridDim.x) {
-        if (seen_of<F::TILE>(a, r).tiles) continue;
-        for (uint32_t i = tid; i < a.heads * a.dim; i += kThreads) {
+        if (seen_of(a, r).tiles) continue;
+        for (uint32_t i = lane; i < a.heads * a.dim; i += 64u) {
             const uint32_t h = i / a.dim;
             reinterpret_cast<uint16_t *>(a.out)[(int64_t)r * a.out_token + (int64_t)h * a.out_head + (i - h * a.dim)] = 0;
         }
         if (a.lse)
-            for (uint32_t h = tid; h < a.heads; h += kThreads) a.lse[(int64_t)r * a.heads + h] = -INFINITY;
+            for (uint32_t h = lane; h < a.heads; h += 64u) a.lse[(int64_t)r * a.heads + h] = -INFINITY;
+        if (a.splits)
+            for (uint32_t i = lane; i < a.segments; i += 64u) a.splits[r * a.segments + i] = Split{0u, 0u};
     }
-    Split *const split = reinterpret_cast<Split *>(a.parts) + blockIdx.x;
-    float *const parts = a.parts + gridDim.x * (sizeof(Split) / 4);
+    if (u >= end) return;
     constexpr uint32_t kPart = kColumns * (F::DP + 2);   // maxima, sums, results of one piece of a segment
-    if (u >= end) {
-        if (a.parts && tid == 0) *split = Split{0, 0, 0, 0};
-        return;
-    }
+    // the request of the first unit: the lane whose run holds it, then the request in its run
+    const uint32_t want = fdiv(u, a.by_segments);
+    uint32_t r, first_of;
     {
-        const uint32_t want = fdiv(u, a.by_segments);
-        uint32_t before = 0;
-        for (uint32_t r0 = 0;; r0 += kThreads) {   // (ends: `want` is under the sum of all)
-            const uint32_t r = r0 + tid, n = r < a.requests ? seen_of<F::TILE>(a, r).tiles : 0u;
-            uint32_t x = n;
-#pragma unroll
-            for (uint32_t d = 1; d < 64; d <<= 1) {
-                const uint32_t y = __shfl_up(x, d);
-                if (lane >= d) x += y;
+        const uint32_t at = (uint32_t)__builtin_ctzll(__ballot(want < upto));   // (there is one: `want` is under the sum of all)
+        uint32_t before = __builtin_amdgcn_readlane(upto - tiles, at);
+        r = at * run;
+        first_of = before * a.segments;   // the request's first unit
+        for (; run > 1; r += 64u) {
+            const uint32_t mine = r + lane, n = mine < a.requests ? seen_of(a, mine).tiles : 0u, x = before + sum_up_to(n, lane);
+            const uint64_t in = __ballot(want < x);
+            if (in) {
+                const uint32_t of = (uint32_t)__builtin_ctzll(in);
+                r += of;
+                first_of = __builtin_amdgcn_readlane(x - n, of) * a.segments;
+                break;
             }
-            __syncthreads();
-            if (lane == 63) sums[wave] = x;
-            __syncthreads();
-            uint32_t to = before;
-            for (uint32_t w = 0; w < F::WAVES; ++w) {
-                if (w == wave) x += to;
-                to += sums[w];
-            }
-            if (want >= x - n && want < x) found[0] = r, found[1] = x - n;
-            before = to;
-            if (want < to) break;
+            before = __builtin_amdgcn_readlane(x, 63);
         }
-        __syncthreads();
     }
-    uint32_t r = __builtin_amdgcn_readfirstlane(found[0]);
-    uint32_t first_of = __builtin_amdgcn_readfirstlane(found[1]) * a.segments;   // the request's first unit
-    Seen seen = seen_of<F::TILE>(a, r);
+    Seen seen = seen_of(a, r);
     uint32_t segment = (u - first_of) / seen.tiles, tile = u - first_of - segment * seen.tiles;
-    bool leads_on = false;
 
-    // ---- what does not change from segment to segment
-    uint32_t row_of[F::LOADS], k_piece[F::LOADS], v_piece[F::LOADS];   // of the 16 bytes that this lane loads
+    // ---- what does not change from segment to segment: of the 16 bytes that this lane loads, the row (as an address of ds_bpermute), the piece of
+    // it, and both as an offset in half a tile of one page
+    uint32_t row_of[F::LOADS], k_piece[F::LOADS], v_piece[F::LOADS], k_off[F::LOADS], v_off[F::LOADS];
 #pragma unroll
     for (int j = 0; j < F::LOADS; ++j) {
         const uint32_t i = 64u * j + lane, row = i / F::NC, at = i % F::NC;
-        row_of[j] = 4u * row;   // (as a byte address of ds_bpermute)
+        row_of[j] = 4u * row;
         k_piece[j] = at ^ key_swizzle<F>(row);
         v_piece[j] = at ^ value_swizzle<F>(row);
+        k_off[j] = (((row & 15u) * a.token_step + k_piece[j]) << 4) + 4096u - 1024u * (j & 3);
+        v_off[j] = (((row & 15u) * a.token_step + v_piece[j]) << 4) + 4096u - 1024u * (j & 3);
+    }
+    // where this lane's parts of a stage lie
+    uint32_t k_at[2][F::DP / 32], v_at[2][F::DP / 16];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const uint32_t token = 8u * (col >> 2) + 4u * t + (col & 3u);
+#pragma unroll
+        for (int i = 0; i < F::DP / 32; ++i)
+            k_at[t][i] = base + token * F::ROW +
+                         (F::ES == 2 ? ((4u * i + g) ^ key_swizzle<F>(token)) << 4 : (((2u * i + (g >> 1)) ^ key_swizzle<F>(token)) << 4) + ((g & 1u) << 3));
+#pragma unroll
+        for (int i = 0; i < F::DP / 16; ++i) {
+            const uint32_t row = F::ES == 2 ? 8u * g + (col >> 2) + 4u * t : 8u * g + (col >> 1);   // (8-bit: one access, t unused)
+            v_at[t][i] = base + F::SIDE + row * F::ROW +
+                         (F::ES == 2 ? ((2u * i + ((col & 3u) >> 1)) ^ value_swizzle<F>(row)) << 4 : ((uint32_t)i ^ value_swizzle<F>(row)) << 4) + ((col & 1u) << 3);
+        }
     }
 
     while (u < end) {
@@ -272,44 +301,58 @@ __global__ __launch_bounds__(64 * F::WAVES, F::PER_UNIT) void amap_attend_kernel
         const uint32_t q0 = block * a.columns, rows = min(a.group - q0, a.columns);   // queries of the block
         const uint32_t head0 = kv * a.group + q0;
 
-        // ---- a wavefront's steps: its 32 tokens of every tile that hold a visible one
-        const uint32_t t0 = (seen.tile + tile) * F::TILE + wave * kTokens;
-        const uint32_t s0 = t0 + kTokens <= seen.first ? 1u : 0u;
-        const uint32_t s1 = t0 + (n - 1) * F::TILE >= seen.past ? n - 1 : n;
-        const uint32_t steps = s1 > s0 ? s1 - s0 : 0u, begin = t0 + s0 * F::TILE;
+        const uint32_t begin = (seen.tile + tile) * kTokens, steps = n;
         const int32_t *const row = a.table + (int64_t)r * a.table_stride;
-        constexpr int L = 2 * F::LOADS + 1;   // loads of a step
-        uint32_t mask[F::STAGES];   // of each stage's visible tokens
+        constexpr int LV = F::LOADS, LK = LV + 1;   // loads of a step's values; of its keys and the pages of the step after next
         auto ask = [&](uint32_t s, uint32_t slot) __attribute__((always_inline)) {   // the pages of step s
-            const uint32_t token = min(max(begin + s * F::TILE + (lane & 31u), seen.first), seen.past - 1u);
+            const uint32_t token = min(max(begin + s * kTokens + (lane & 31u), seen.first), seen.past - 1u);
             load4(row + fdiv(token, a.by_page), ids + slot * 256u);
         };
-        auto issue = [&](uint32_t s, uint32_t slot) __attribute__((always_inline)) {   // -> the mask
-            const uint32_t token = begin + s * F::TILE + (lane & 31u);
+        uint32_t shown[2];    // of each stage, which tokens are visible
+        uint32_t places = 0;  // of the step being loaded: where this lane's token lies (kNoRow: nowhere), in 16-byte pieces,
+        bool fast = false;    // or, all of them being visible, where either half of them begins
+        int64_t lo = 0, hi = 0;
+        const char *const zeros = reinterpret_cast<const char *>(&kZeros);
+        auto load_side = [&](const char *from, const uint32_t (&off)[F::LOADS], const uint32_t (&piece)[F::LOADS], uint32_t lds) __attribute__((always_inline)) {
+            if (fast) {
+                load_rows<F::LOADS>(from + lo, from + hi, off, lds);
+            } else {
+                uint32_t x[F::LOADS];
+#pragma unroll
+                for (int i = 0; i < F::LOADS; ++i) x[i] = (uint32_t)__builtin_amdgcn_ds_bpermute((int)row_of[i], (int)places);
+#pragma unroll
+                for (int i = 0; i < F::LOADS; ++i)
+                    load16(x[i] != kNoRow && piece[i] < a.pieces ? from + ((uint64_t)(x[i] + piece[i]) << 4) : zeros, lds + 1024u * i);
+            }
+        };
+        auto load_keys = [&](uint32_t s, int slot) __attribute__((always_inline)) {
+            const uint32_t t0 = begin + s * kTokens, token = t0 + (lane & 31u);
             const uint32_t id = lds_at<uint32_t>(ids + slot * 256u + 4u * (lane & 31u));
             const bool there = token >= seen.first && token < seen.past && id < a.n_pages;
-            const uint32_t j = fdiv(token, a.by_page);
-            const uint32_t at = there ? id * a.page_step + (token - j * a.page) * a.token_step + kv * a.head_step : kNoRow;
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this stage has been read, and its ids
-            const uint32_t lds = base + slot * F::STAGE;
-            const char *const none = reinterpret_cast<const char *>(&kZeros);
-            uint32_t off[F::LOADS];
-#pragma unroll
-            for (int i = 0; i < F::LOADS; ++i) off[i] = (uint32_t)__builtin_amdgcn_ds_bpermute((int)row_of[i], (int)at);
-#pragma unroll
-            for (int i = 0; i < F::LOADS; ++i)
-                load16(off[i] != kNoRow && k_piece[i] < a.pieces ? a.k + ((uint64_t)(off[i] + k_piece[i]) << 4) : none, lds + 1024u * i);
-            if constexpr (F::STAGES * L > 63) landed<63 - (F::LOADS + 1)>();   // no more than the counter holds
-#pragma unroll
-            for (int i = 0; i < F::LOADS; ++i)
-                load16(off[i] != kNoRow && v_piece[i] < a.pieces ? a.v + ((uint64_t)(off[i] + v_piece[i]) << 4) : none, lds + F::SIDE + 1024u * i);
-            ask(s + F::STAGES, slot);
-            return (uint32_t)__ballot(there);
+            shown[slot] = (uint32_t)__ballot(there);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the keys that were here have been read, and the pages
+            if constexpr (2 * LV + LK + LK > 63) landed<63 - LK>();   // no more than the counter holds
+            fast = F::HALVES && a.halves && shown[slot] == 0xFFFFFFFFu;
+            if (fast) {
+                const uint32_t j0 = fdiv(t0, a.by_page), j1 = fdiv(t0 + 16u, a.by_page), id0 = __builtin_amdgcn_readlane(id, 0), id1 = __builtin_amdgcn_readlane(id, 16);
+                const uint32_t x0 = id0 * a.page_step + (t0 - j0 * a.page) * a.token_step + kv * a.head_step;
+                const uint32_t x1 = id1 * a.page_step + (t0 + 16u - j1 * a.page) * a.token_step + kv * a.head_step;
+                lo = ((int64_t)x0 << 4) - 4096;
+                hi = ((int64_t)x1 << 4) - 4096;
+            } else {
+                const uint32_t j = fdiv(token, a.by_page);
+                places = there ? id * a.page_step + (token - j * a.page) * a.token_step + kv * a.head_step : kNoRow;
+            }
+            load_side(a.k, k_off, k_piece, base + slot * F::STAGE);
+            ask(s + 2, slot);
         };
-        if (steps) {
+        auto load_values = [&](int slot) __attribute__((always_inline)) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the values that were here have been read
+            if constexpr (LV + LK + LK + LV > 63) landed<63 - LV>();
+            load_side(a.v, v_off, v_piece, base + F::SIDE + slot * F::STAGE);
+        };
 #pragma unroll
-            for (int s = 0; s < F::STAGES; ++s) ask(s, s);
-        }
+        for (int s = 0; s < 2; ++s) ask(s, s);
         // the queries: column c is query c, or c % 8 where the weights' second parts have columns 8 .. 15
         eight qf[F::DP / 32];
         {
@@ -341,42 +384,45 @@ __global__ __launch_bounds__(64 * F::WAVES, F::PER_UNIT) void amap_attend_kernel
 #pragma unroll
         for (int i = 0; i < F::DP / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
-        if (steps) {
-            landed<0>();   // the first pages, and the queries
-#pragma unroll
-            for (int s = 0; s < F::STAGES; ++s) mask[s] = (uint32_t)s < steps ? issue(s, s) : 0u;
+        landed<0>();   // the first pages, and the queries
+        load_keys(0, 0);
+        load_values(0);
+        if (steps > 1) {
+            load_keys(1, 1);
+            load_values(1);
         }
-        for (uint32_t s = 0, slot = 0; s < steps; ++s) {
-            landed_but<L, F::STAGES - 1>(steps - 1u - s);
-            const uint32_t k_at = base + slot * F::STAGE, v_at = k_at + F::SIDE, shown = mask[0];
+        auto step = [&](uint32_t s, auto stage) __attribute__((always_inline)) {
+            constexpr int slot = decltype(stage)::value;
+            const bool next = s + 1 < steps, after = s + 2 < steps;
+            if (next)
+                landed<2 * LV + LK>();
+            else
+                landed<LV>();
             // ---- scores: this lane's are of column `col` and tokens 8 g .. 8 g + 7
             f32x4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t token = 8u * (col >> 2) + 4u * t + (col & 3u);
+            for (int i = 0; i < F::DP / 32; ++i)
 #pragma unroll
-                for (int i = 0; i < F::DP / 32; ++i) {
+                for (int t = 0; t < 2; ++t) {
                     eight kf;
-                    if constexpr (F::ES == 2) {
-                        kf = lds_at<eight>(k_at + token * F::ROW + (((4u * i + g) ^ key_swizzle<F>(token)) << 4));
-                    } else {
-                        kf = eight_of_e4m3<typename F::T>(lds_at<u32x2>(k_at + token * F::ROW + (((2u * i + (g >> 1)) ^ key_swizzle<F>(token)) << 4) + ((g & 1u) << 3)));
-                    }
+                    if constexpr (F::ES == 2)
+                        kf = lds_at<eight>(k_at[t][i] + slot * F::STAGE);
+                    else
+                        kf = eight_of_e4m3<typename F::T>(lds_at<u32x2>(k_at[t][i] + slot * F::STAGE));
                     c[t] = Of<typename F::T>::product(kf, qf[i], c[t]);
                 }
-            }
+            const uint32_t visible = shown[slot];
+            if (after) load_keys(s + 2, slot);
             float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = c[j >> 2][j & 3] * by;
-            if (shown != 0xFFFFFFFFu) {
-                const uint32_t mine = shown >> (8u * g);
+            if (visible != 0xFFFFFFFFu) {
+                const uint32_t mine = visible >> (8u * g);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = mine >> j & 1u ? x[j] : -INFINITY;
             }
             float high = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            high = fmaxf(high, __shfl_xor(high, 16));
-            high = fmaxf(high, __shfl_xor(high, 32));
-            high = fmaxf(high, m);
+            high = fmaxf(top_of_column(high), m);
             const float from = high == -INFINITY ? 0.f : high;
             if (__any(high != m)) {
                 const float keep = __builtin_amdgcn_exp2f(m - from);
@@ -400,167 +446,172 @@ __global__ __launch_bounds__(64 * F::WAVES, F::PER_UNIT) void amap_attend_kernel
                 if (col >= 8u) pf = rest;
             }
             // ---- results: 16 elements of V's rows at a time
+            if (after)
+                landed<2 * LK + LV>();
+            else if (next)
+                landed<LK + LV>();
+            else
+                landed<0>();
 #pragma unroll
             for (int i = 0; i < F::DP / 16; ++i) {
                 eight vf;
                 if constexpr (F::ES == 2) {
-                    const uint32_t r0 = 8u * g + (col >> 2), in = (col & 3u) << 3;
                     union {
                         i16x4 half[2];
                         eight whole;
                     } y;
 #pragma unroll
-                    for (int hi = 0; hi < 2; ++hi) {
-                        const uint32_t at = v_at + (r0 + 4u * hi) * F::ROW + (((2u * i + (in >> 4)) ^ value_swizzle<F>(r0 + 4u * hi)) << 4) + (in & 8u);
-                        y.half[hi] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_char *)(uintptr_t)at);
-                    }
+                    for (int t = 0; t < 2; ++t)
+                        y.half[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_char *)(uintptr_t)(v_at[t][i] + slot * F::STAGE));
                     vf = y.whole;
                 } else {
-                    const uint32_t r0 = 8u * g + (col >> 1);
-                    const uint32_t at = v_at + r0 * F::ROW + (((uint32_t)i ^ value_swizzle<F>(r0)) << 4) + ((col & 1u) << 3);
-                    vf = eight_of_e4m3<typename F::T>(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(lds_char *)(uintptr_t)at)));
+                    vf = eight_of_e4m3<typename F::T>(__builtin_bit_cast(
+                        u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(lds_char *)(uintptr_t)(v_at[0][i] + slot * F::STAGE))));
                 }
                 o[i] = Of<typename F::T>::product(vf, pf, o[i]);
                 if constexpr (!F::PAIRED) o[i] = Of<typename F::T>::product(vf, rest, o[i]);
             }
-#pragma unroll
-            for (int i = 0; i + 1 < F::STAGES; ++i) mask[i] = mask[i + 1];
-            mask[F::STAGES - 1] = s + F::STAGES < steps ? issue(s + F::STAGES, slot) : 0u;
-            slot = slot + 1 == F::STAGES ? 0u : slot + 1;
+            if (after) load_values(slot);
+        };
+        for (uint32_t s = 0; s < steps; s += 2) {
+            step(s, std::integral_constant<int, 0>{});
+            if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{});
         }
-        landed<0>();   // (pages asked for that no step needs)
 
-        // ---- the wavefronts' results side by side, in the place of their stages
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (g == 0) top[wave][col] = m, total[wave][col] = l;
+        // ---- the results, through LDS (in the place of the stages) into rows; a piece of a segment into the workspace
+        l = sum_of_column(l);
+        const bool whole = tile == 0 && n == seen.tiles, none = l == 0.f;   // (none: scores of -inf only)
+        float *const part = a.parts + (size_t)(2u * blockIdx.x + (tile == 0)) * kPart;   // the first piece of a segment, or a later one
+        const float vs = whole ? (none ? 0.f : (a.v_scale ? a.v_scale[kv] : 1.f) / l) : 1.f;
+        if (lane < rows) {
+            if (!whole)
+                part[lane] = m, part[kColumns + lane] = l;
+            else if (a.lse)
+                a.lse[(int64_t)r * a.heads + head0 + lane] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        }
 #pragma unroll
-        for (int i = 0; i < F::DP / 16; ++i) lds_put<f32x4>(base + 4u * (col * F::OUT_ROW + 16u * i + 4u * g), o[i]);
-        __syncthreads();
-        const bool whole = tile == 0 && n == seen.tiles;
-        const float vs = a.v_scale ? a.v_scale[kv] : 1.f;
-        float *const part = parts + (size_t)(2u * blockIdx.x + (tile == 0)) * kPart;   // the first piece of a segment, or a later one
-        const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char *)smem;
-        for (uint32_t i = tid; i < rows * F::DP; i += kThreads) {
-            const uint32_t c = i / F::DP, d = i - c * F::DP;
-            float high = top[0][c];
-#pragma unroll
-            for (int w = 1; w < F::WAVES; ++w) high = fmaxf(high, top[w][c]);
-            const float from = high == -INFINITY ? 0.f : high;
-            float sum = 0.f, x = 0.f;
-#pragma unroll
-            for (int w = 0; w < F::WAVES; ++w) {
-                const float keep = __builtin_amdgcn_exp2f(top[w][c] - from);
-                const uint32_t at = lds0 + w * F::PER_WAVE + 4u * (c * F::OUT_ROW + d);
-                float y = lds_at<float>(at);
-                if constexpr (F::PAIRED) y += lds_at<float>(at + 4u * 8u * F::OUT_ROW);
-                sum += keep * total[w][c];
-                x += keep * y;
-            }
-            if (whole) {
-                const bool none = sum == 0.f;   // (scores of -inf only)
-                if (d < a.dim) {
-                    const float y = none ? 0.f : x * vs / sum;
-                    reinterpret_cast<typename Of<typename F::T>::one *>(a.out)[(int64_t)r * a.out_token + (int64_t)(head0 + c) * a.out_head + d] =
-                        (typename Of<typename F::T>::one)y;
-                }
-                if (d == 0 && a.lse) a.lse[(int64_t)r * a.heads + head0 + c] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
+        for (int i = 0; i < F::DP / 16; ++i) lds_put<f32x4>(base + 4u * (col * F::OUT_ROW + 16u * i + 4u * g), none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[i] * vs);
+        for (uint32_t i = lane; i < rows * (F::DP / 4); i += 64u) {
+            const uint32_t c = i / (F::DP / 4), d = 4u * (i % (F::DP / 4)), at = base + 4u * (c * F::OUT_ROW + d);
+            f32x4 x = lds_at<f32x4>(at);
+            if constexpr (F::PAIRED) x += lds_at<f32x4>(at + 4u * 8u * F::OUT_ROW);
+            if (!whole) {
+                *reinterpret_cast<f32x4 *>(part + 2 * kColumns + 4 * i) = x;
             } else {
-                part[2 * kColumns + i] = x;
-                if (d == 0) part[c] = high, part[kColumns + c] = sum;
+                typename Of<typename F::T>::one *const out =
+                    reinterpret_cast<typename Of<typename F::T>::one *>(a.out) + (int64_t)r * a.out_token + (int64_t)(head0 + c) * a.out_head + d;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (d + e < a.dim) out[e] = (typename Of<typename F::T>::one)x[e];
             }
         }
-        __syncthreads();
-        if (!whole && tile == 0) {
-            leads_on = true;
-            if (tid == 0) *split = Split{r, segment, (u + seen.tiles - 1) / share - blockIdx.x + 1, 0};
-        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, before the next segment's loads land there
+        if (a.splits && tile == 0 && lane == 0) a.splits[r * a.segments + segment] = Split{blockIdx.x, whole ? 0u : (u + seen.tiles - 1) / share - blockIdx.x + 1};
         u += n;
         tile = 0;
         if (++segment == a.segments) {
             segment = 0;
             if (u < end) do
-                    seen = seen_of<F::TILE>(a, ++r);
+                    seen = seen_of(a, ++r);
                 while (seen.tiles == 0);   // (there is one: units are left)
         }
     }
-    if (a.parts && !leads_on && tid == 0) *split = Split{0, 0, 0, 0};
 }
 
-// The pieces of a segment that was cut, joined: one workgroup per row of a segment, found at the workgroup in whose share it began.
+// The segments that were cut, their pieces joined: a segment (all its rows at once) or one row of it to a workgroup.
 struct JoinArgs {
     const float *parts;
+    const Split *splits;
     char *out;
     float *lse;
     const float *v_scale;
     int64_t out_token, out_head;
-    uint32_t groups, columns, group, heads, dim, blocks;
-    FastDiv by_columns, by_blocks;
+    uint32_t work, rows, columns, group, heads, dim;   // rows: row blocks of a segment, 1 or `columns`
+    FastDiv by_rows, by_segments, by_blocks;
+    uint32_t segments, blocks;
 };
 
 template <class T, int DP>
 __global__ __launch_bounds__(256) void amap_attend_join_kernel(const JoinArgs a) {
-    constexpr uint32_t kPart = kColumns * (DP + 2), kLanes = DP / 4, kAtOnce = 256 / kLanes;
-    __shared__ float sums[kAtOnce];
-    __shared__ f32x4 results[kAtOnce][kLanes];
-    const uint32_t w = fdiv(blockIdx.x, a.by_columns), c = blockIdx.x - w * a.columns;
-    const Split s = reinterpret_cast<const Split *>(a.parts)[w];
-    const uint32_t kv = fdiv(s.segment, a.by_blocks), block = s.segment - kv * a.blocks;
-    if (s.count == 0 || c >= min(a.group - block * a.columns, a.columns)) return;
-    const float *const parts = a.parts + a.groups * (sizeof(Split) / 4) + (size_t)(2u * w) * kPart;
-    auto at = [&](uint32_t i) { return parts + (size_t)(i ? 2u * i : 1u) * kPart; };
-    const uint32_t tid = threadIdx.x, from = tid / kLanes, d = 4u * (tid % kLanes);
-    float high = -INFINITY;
-    for (uint32_t i = 0; i < s.count; ++i) high = fmaxf(high, at(i)[c]);
-    const float base = high == -INFINITY ? 0.f : high;
-    float sum = 0.f;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (from < kAtOnce)
-        for (uint32_t i = from; i < s.count; i += kAtOnce) {
-            const float *const p = at(i);
-            const float keep = __builtin_amdgcn_exp2f(p[c] - base);
-            sum += keep * p[kColumns + c];
-            x += keep * *reinterpret_cast<const f32x4 *>(p + 2 * kColumns + c * DP + d);
-        }
-    if (from < kAtOnce) {
-        results[from][tid % kLanes] = x;
-        if (tid % kLanes == 0) sums[from] = sum;
-    }
-    __syncthreads();
-    if (from) return;
-    for (uint32_t i = 1; i < kAtOnce; ++i) {
-        sum += sums[i];
-        x += results[i][tid];
-    }
-    const bool none = sum == 0.f;
-    const uint32_t h = kv * a.group + block * a.columns + c;
-    const float vs = a.v_scale ? a.v_scale[kv] : 1.f;
-    typename Of<T>::one *const out = reinterpret_cast<typename Of<T>::one *>(a.out) + (int64_t)s.request * a.out_token + (int64_t)h * a.out_head;
+    constexpr uint32_t kPart = kColumns * (DP + 2), kLanes = DP / 4, kSlots = 256 / kLanes;   // slots: of a row's lanes
+    __shared__ float tops[kSlots], sums[kSlots];
+    __shared__ f32x4 results[kSlots][kLanes];
+    const uint32_t slot = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, d = 4u * lane;
+    for (uint32_t i = blockIdx.x; i < a.work; i += gridDim.x) {
+        const uint32_t id = fdiv(i, a.by_rows), row_block = i - id * a.rows;
+        const Split s = a.splits[id];
+        if (s.count == 0) continue;
+        const uint32_t r = fdiv(id, a.by_segments), segment = id - r * a.segments;
+        const uint32_t kv = fdiv(segment, a.by_blocks), block = segment - kv * a.blocks, rows = min(a.group - block * a.columns, a.columns);
+        // a slot has one row of so many at once, and every so-manieth piece of it
+        const uint32_t at_once = a.rows > 1 ? 1u : min(rows, kSlots), ways = kSlots / at_once, way = slot / at_once;
+        const float *const first = a.parts + (size_t)(2u * s.group) * kPart;
+        for (uint32_t c0 = row_block; c0 < (a.rows > 1 ? min(row_block + 1, rows) : rows); c0 += at_once) {
+            const uint32_t c = c0 + slot % at_once;
+            float high = -INFINITY, sum = 0.f;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            if (way < ways && c < rows) {
+#pragma unroll 4
+                for (uint32_t p = way; p < s.count; p += ways) {
+                    const float *const part = first + (size_t)(p ? 2u * p : 1u) * kPart;
+                    const float m = part[c], l = part[kColumns + c];
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(part + 2 * kColumns + c * DP + d);
+                    const float up = fmaxf(high, m), base = up == -INFINITY ? 0.f : up;
+                    const float keep = __builtin_amdgcn_exp2f(high - base), take = __builtin_amdgcn_exp2f(m - base);
+                    sum = sum * keep + l * take;
+                    x = x * keep + y * take;
+                    high = up;
+                }
+            }
+            if (slot < kSlots) {
+                results[slot][lane] = x;
+                if (lane == 0) tops[slot] = high, sums[slot] = sum;
+            }
+            __syncthreads();
+            if (way == 0 && c < rows) {
+                for (uint32_t w = 1; w < ways; ++w) {
+                    const uint32_t other = slot + w * at_once;
+                    const float m = tops[other], up = fmaxf(high, m), base = up == -INFINITY ? 0.f : up;
+                    const float keep = __builtin_amdgcn_exp2f(high - base), take = __builtin_amdgcn_exp2f(m - base);
+                    sum = sum * keep + sums[other] * take;
+                    x = x * keep + results[other][lane] * take;
+                    high = up;
+                }
+                const bool none = sum == 0.f;
+                const uint32_t h = kv * a.group + block * a.columns + c;
+                const float by = none ? 0.f : (a.v_scale ? a.v_scale[kv] : 1.f) / sum;
+                typename Of<T>::one *const out = reinterpret_cast<typename Of<T>::one *>(a.out) + (int64_t)r * a.out_token + (int64_t)h * a.out_head;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (d + e < a.dim) out[d + e] = (typename Of<T>::one)(none ? 0.f : x[e] * vs / sum);
-    if (tid == 0 && a.lse) a.lse[(int64_t)s.request * a.heads + h] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
+                for (int e = 0; e < 4; ++e)
+                    if (d + e < a.dim) out[d + e] = (typename Of<T>::one)(none ? 0.f : x[e] * by);
+                if (lane == 0 && a.lse) a.lse[(int64_t)r * a.heads + h] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
+            }
+            __syncthreads();
+        }
+    }
 }
 
 // How a call is cut: workgroups, columns of a block, and whether a segment may be split between workgroups.
 struct Cut {
-    uint32_t groups, columns, blocks, segments, tile;
+    uint32_t groups, columns, blocks, segments;
     bool splits;
     int dp;
-    int64_t bytes;
+    int64_t parts, bytes;   // where the pieces begin in the workspace, and its size
 };
 
 template <class F>
 amap_status attend(AttendArgs a, const Cut &cut, hipStream_t s) {
-    static LdsReservation reserved;
-    if constexpr (F::LDS > 65536 - 1024) {
+    if constexpr (F::LDS > 65536) {
+        static LdsReservation reserved;
         const hipError_t e = reserved.on_current_device({reinterpret_cast<const void *>(amap_attend_kernel<F>)}, F::LDS);
         if (e != hipSuccess) return launched(e, "amap_attend_kernel: cannot reserve its LDS stages");
     }
-    hipError_t e = launch_kernel<amap_attend_kernel<F>>(dim3(cut.groups), dim3(64 * F::WAVES), F::LDS, s, a);
+    hipError_t e = launch_kernel<amap_attend_kernel<F>>(dim3(cut.groups), dim3(64), F::LDS, s, a);
     if (e != hipSuccess || !cut.splits) return launched(e, "amap_attend_kernel");
-    const JoinArgs j{a.parts, a.out, a.lse, a.v_scale, a.out_token, a.out_head, cut.groups, a.columns, a.group, a.heads, a.dim, a.blocks, make_fastdiv(a.columns), a.by_blocks};
-    e = launch_kernel<amap_attend_join_kernel<typename F::T, F::DP>>(dim3(cut.groups * a.columns), dim3(256), 0, s, j);
+    const uint32_t segments = a.requests * a.segments, rows = segments <= kFewSegments ? a.columns : 1u, work = segments * rows;
+    const JoinArgs j{a.parts, a.splits, a.out, a.lse, a.v_scale, a.out_token, a.out_head, work, rows, a.columns, a.group, a.heads, a.dim, make_fastdiv(rows), a.by_segments, a.by_blocks,
+                     a.segments, a.blocks};
+    e = launch_kernel<amap_attend_join_kernel<typename F::T, F::DP>>(dim3(work < kMostJoining ? work : kMostJoining), dim3(256), 0, s, j);
     return launched(e, "amap_attend_join_kernel");
 }
 
@@ -606,15 +657,15 @@ amap_status cut_of(const amap_cache &c, int heads, int64_t requests, int table_w
     cut.segments = cut.blocks * (uint32_t)c.kv_heads;
     uint32_t per_unit = 1;
     with_form(AMAP_BF16, c.type, cut.dp, group <= 8, [&](auto form) {
-        cut.tile = decltype(form)::TILE;
         per_unit = decltype(form)::PER_UNIT;
     });
-    const int64_t tiles = ((int64_t)table_width * c.page_size + cut.tile - 1) / cut.tile;
+    const int64_t tiles = ((int64_t)table_width * c.page_size + kTokens - 1) / kTokens;
     int64_t most;
     if (__builtin_mul_overflow(requests * cut.segments, tiles, &most) || most >= ((int64_t)1 << 31)) return refuse("2^31 tiles of tokens or more over all requests and key heads");
     cut.splits = tiles > 1;
     cut.groups = (uint32_t)(most < 1 ? 1 : most < kUnits * per_unit ? most : kUnits * per_unit);
-    cut.bytes = cut.splits ? (int64_t)cut.groups * (int64_t)(sizeof(Split) + 2 * 4 * kColumns * (cut.dp + 2)) : 0;
+    cut.parts = (requests * cut.segments * (int64_t)sizeof(Split) + 15) / 16 * 16;
+    cut.bytes = cut.splits ? cut.parts + (int64_t)cut.groups * (2 * 4 * kColumns * (cut.dp + 2)) : 0;
     return AMAP_OK;
 }
 
@@ -661,7 +712,10 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     a.q = static_cast<const char *>(q->data);
     a.out = static_cast<char *>(out->data);
     a.lse = lse;
-    a.parts = cut.splits ? static_cast<float *>(workspace) : nullptr;
+    if (cut.splits) {
+        a.splits = static_cast<Split *>(workspace);
+        a.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + cut.parts);
+    }
     a.k_scale = cache->k_scale;
     a.v_scale = cache->v_scale;
     a.table = table;
@@ -693,6 +747,8 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     a.least = 1;
     a.window = (uint32_t)window;
     a.aligned = q_at % 16 == 0 && (requests == 1 || q->token_stride % 8 == 0) && (q->heads == 1 || q->head_stride % 8 == 0);
+    // (16 rows of a page within 32-bit byte offsets; heads of a whole form: no pieces of zeros)
+    a.halves = cache->page_size % 16 == 0 && dim == cut.dp && (cache->page_size == 1 || cache->token_stride * es * 16 < ((int64_t)1 << 31));
     a.scale = scale;
     with_form(q->type, cache->type, cut.dp, cut.columns == 8, [&](auto form) { st = attend<decltype(form)>(a, cut, s); });
     return st;
