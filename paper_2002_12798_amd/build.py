@@ -75,8 +75,8 @@ def build_call():
             os.remove(CALL)   # of another state of the source
         print(f"{CALL} not built (no {lacks}): Python calls go through ctypes", file=sys.stderr)
         return None
-    subprocess.run(["gcc", "-O2", "-std=c99", "-fPIC", "-shared", "-Wall", "-Wextra", "-I", include,
-                    os.path.join(CSRC, "amap_call.c"), "-o", CALL], check=True)
+    subprocess.run(["gcc", "-O2", "-std=c99", "-fPIC", "-shared", "-Wall", "-Wextra", "-I", include, "-I", os.path.join(ROOT, "include"),
+                    os.path.join(CSRC, "amap_call.c"), "-o", CALL, "-lm"], check=True)
     untagged = os.path.join(_HERE, "_amap_call.so")   # built so before: any interpreter would load it
     if os.path.exists(untagged):
         os.remove(untagged)

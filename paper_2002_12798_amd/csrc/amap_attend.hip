@@ -29,6 +29,7 @@ constexpr uint32_t kUnits = 256;   // compute units of an MI355X
 constexpr int kTokens = 32;        // of a wavefront's step
 constexpr int kColumns = 16;       // queries of a workgroup at a time (8 where their weights' second parts have the others)
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
+constexpr uint32_t kBegin = 3;             // what beginning and ending a segment counts for in a share, in tiles
 constexpr uint32_t kFewSegments = 128;     // up to so many are joined row by row: they are in many pieces each
 constexpr uint32_t kMostJoining = 4096;    // workgroups of a join
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
@@ -195,7 +196,7 @@ __device__ __forceinline__ void lds_put(uint32_t at, X x) {
 
 // the visible tokens of a request, and the tiles that hold them
 struct Seen {
-    uint32_t first, past, tile, tiles;
+    uint32_t first, past, tile, tiles, units;   // units: its tiles and what a segment of them costs besides
 };
 __device__ __forceinline__ Seen seen_of(const AttendArgs &a, uint32_t r) {
     Seen s;
@@ -203,6 +204,7 @@ __device__ __forceinline__ Seen seen_of(const AttendArgs &a, uint32_t r) {
     s.first = a.window && s.past > a.window ? s.past - a.window : 0u;
     s.tile = s.first / kTokens;
     s.tiles = (s.past + kTokens - 1) / kTokens - s.tile;
+    s.units = s.tiles ? s.tiles + kBegin : 0u;
     return s;
 }
 __device__ __forceinline__ uint32_t sum_up_to(uint32_t x, uint32_t lane) {   // over the lanes, this one's included
@@ -215,7 +217,7 @@ __device__ __forceinline__ uint32_t sum_up_to(uint32_t x, uint32_t lane) {   // 
 }
 
 template <class F>
-__global__ __launch_bounds__(64) void amap_attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(const AttendArgs a) {
     typedef typename Of<typename F::T>::eight eight;
     extern __shared__ char smem[];
     const uint32_t lane = threadIdx.x, g = lane >> 4, col = lane & 15u;
@@ -223,9 +225,9 @@ __global__ __launch_bounds__(64) void amap_attend_kernel(const AttendArgs a) {
 
     // ---- the share: tiles of all requests, an equal run of them to a lane
     const uint32_t run = (a.requests + 63u) >> 6, r0 = min(lane * run, a.requests), r1 = min(r0 + run, a.requests);
-    uint32_t tiles = 0;
-    for (uint32_t r = r0; r < r1; ++r) tiles += seen_of(a, r).tiles;
-    const uint32_t upto = sum_up_to(tiles, lane), all = __builtin_amdgcn_readlane(upto, 63) * a.segments;
+    uint32_t units = 0;
+    for (uint32_t r = r0; r < r1; ++r) units += seen_of(a, r).units;
+    const uint32_t upto = sum_up_to(units, lane), all = __builtin_amdgcn_readlane(upto, 63) * a.segments;
     const uint32_t share = max(a.least, (all + gridDim.x - 1) / gridDim.x);
     uint32_t u = blockIdx.x * share;
     const uint32_t end = min(u + share, all);
@@ -248,11 +250,11 @@ __global__ __launch_bounds__(64) void amap_attend_kernel(const AttendArgs a) {
     uint32_t r, first_of;
     {
         const uint32_t at = (uint32_t)__builtin_ctzll(__ballot(want < upto));   // (there is one: `want` is under the sum of all)
-        uint32_t before = __builtin_amdgcn_readlane(upto - tiles, at);
+        uint32_t before = __builtin_amdgcn_readlane(upto - units, at);
         r = at * run;
         first_of = before * a.segments;   // the request's first unit
         for (; run > 1; r += 64u) {
-            const uint32_t mine = r + lane, n = mine < a.requests ? seen_of(a, mine).tiles : 0u, x = before + sum_up_to(n, lane);
+            const uint32_t mine = r + lane, n = mine < a.requests ? seen_of(a, mine).units : 0u, x = before + sum_up_to(n, lane);
             const uint64_t in = __ballot(want < x);
             if (in) {
                 const uint32_t of = (uint32_t)__builtin_ctzll(in);
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(64) void amap_attend_kernel(const AttendArgs a) {
         }
     }
     Seen seen = seen_of(a, r);
-    uint32_t segment = (u - first_of) / seen.tiles, tile = u - first_of - segment * seen.tiles;
+    uint32_t segment = (u - first_of) / seen.units, at = u - first_of - segment * seen.units;   // `at`: of the segment's units
 
     // ---- what does not change from segment to segment: of the 16 bytes that this lane loads, the row (as an address of ds_bpermute), the piece of
     // it, and both as an offset in half a tile of one page
@@ -296,7 +298,9 @@ __global__ __launch_bounds__(64) void amap_attend_kernel(const AttendArgs a) {
     }
 
     while (u < end) {
-        const uint32_t n = min(seen.tiles - tile, end - u);   // tiles of this segment's piece
+        // the piece of this segment in the share: its tiles follow the units of its beginning
+        const uint32_t past = min(seen.units, at + (end - u)), tile = at > kBegin ? at - kBegin : 0u, n = past > kBegin ? past - kBegin - tile : 0u;
+        if (n == 0) break;   // (the share ends before the segment's first tile)
         const uint32_t kv = fdiv(segment, a.by_blocks), block = segment - kv * a.blocks;
         const uint32_t q0 = block * a.columns, rows = min(a.group - q0, a.columns);   // queries of the block
         const uint32_t head0 = kv * a.group + q0;
@@ -506,9 +510,9 @@ __global__ __launch_bounds__(64) void amap_attend_kernel(const AttendArgs a) {
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, before the next segment's loads land there
-        if (a.splits && tile == 0 && lane == 0) a.splits[r * a.segments + segment] = Split{blockIdx.x, whole ? 0u : (u + seen.tiles - 1) / share - blockIdx.x + 1};
-        u += n;
-        tile = 0;
+        if (a.splits && tile == 0 && lane == 0) a.splits[r * a.segments + segment] = Split{blockIdx.x, whole ? 0u : (u - at + seen.units - 1) / share - blockIdx.x + 1};
+        u += past - at;
+        at = 0;
         if (++segment == a.segments) {
             segment = 0;
             if (u < end) do
@@ -661,7 +665,7 @@ amap_status cut_of(const amap_cache &c, int heads, int64_t requests, int table_w
     });
     const int64_t tiles = ((int64_t)table_width * c.page_size + kTokens - 1) / kTokens;
     int64_t most;
-    if (__builtin_mul_overflow(requests * cut.segments, tiles, &most) || most >= ((int64_t)1 << 31)) return refuse("2^31 tiles of tokens or more over all requests and key heads");
+    if (__builtin_mul_overflow(requests * cut.segments, tiles + kBegin, &most) || most >= ((int64_t)1 << 31)) return refuse("2^31 tiles of tokens or more over all requests and key heads");
     cut.splits = tiles > 1;
     cut.groups = (uint32_t)(most < 1 ? 1 : most < kUnits * per_unit ? most : kUnits * per_unit);
     cut.parts = (requests * cut.segments * (int64_t)sizeof(Split) + 15) / 16 * 16;

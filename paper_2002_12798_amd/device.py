@@ -3,6 +3,7 @@ libamap.so; nothing here computes, and there is no CPU fallback."""
 from __future__ import annotations
 
 import contextlib
+import operator
 from typing import NamedTuple
 
 import numpy as np
@@ -111,6 +112,14 @@ def gemm_fused(a_src: torch.Tensor, a_map, w: torch.Tensor, out=None, stream=Non
 # (a tensor of 16-bit words holds bf16 bits, as everywhere in this package)
 _ELEMENT = {torch.float32: B.AMAP_F32, torch.bfloat16: B.AMAP_BF16, torch.int16: B.AMAP_BF16, torch.float16: B.AMAP_F16, torch.float8_e4m3fn: B.AMAP_E4M3}
 
+# The ordinary call goes through the extension (its answer is the library's status); what it does not take (-1) goes the long way below, which says why.
+if hasattr(B._L, "amap_rotary"):
+    B._call.paged(*(B.C.cast(getattr(B._L, name), B.C.c_void_p).value for name in ("amap_cache_assign", "amap_rotary", "amap_cache_append", "amap_cache_attend",
+                                                                                   "amap_cache_attend_workspace")),
+                  torch.int32, torch.int64, torch.float32, torch.uint8, tuple(_ELEMENT.items()))
+_rotary, _append, _attend, _assign = B._call.rotary, B._call.append, B._call.attend, B._call.assign
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
+
 
 def _refused(what, why, status=B.AMAP_E_INVALID):
     return B.AmapError(status, f"{what}: {why}")
@@ -140,12 +149,15 @@ class Rope:
     (2p, 2p + 1) if interleaved."""
 
     def __init__(self, freq, axis_pairs=None, interleaved=False):
-        self.freq = _on_gpu(freq, torch.float32, 1, "Rope", "freq")
+        self._freq = _on_gpu(freq, torch.float32, 1, "Rope", "freq")
         self.axis_pairs = (freq.numel(),) if axis_pairs is None else tuple(int(n) for n in axis_pairs)
         self.interleaved = bool(interleaved)
         if not 1 <= len(self.axis_pairs) <= B.AMAP_MAX_AXES or min(self.axis_pairs) < 0 or sum(self.axis_pairs) != freq.numel():
             raise _refused("Rope", f"axis_pairs {self.axis_pairs} are not the {freq.numel()} pairs", B.AMAP_E_SHAPE)
         self._c = B.amap_rope(freq.data_ptr(), freq.numel(), int(self.interleaved), len(self.axis_pairs), (B.C.c_int32 * B.AMAP_MAX_AXES)(*self.axis_pairs))
+        self._rope_at = B.C.addressof(self._c)
+
+    freq = property(operator.attrgetter("_freq"))   # (the library has its address)
 
     def _positions(self, position, tokens, what):
         """The address of [axes, tokens] or [tokens] int32 positions (the latter the same for all axes), and the step between axes."""
@@ -177,13 +189,18 @@ class PagedCache:
         for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             if t is not None and (_on_gpu(t, torch.float32, 1, "PagedCache", name).numel() != k.size(2) or k.dtype != torch.float8_e4m3fn):
                 raise _refused("PagedCache", f"{name} is one scale per head of an 8-bit cache", B.AMAP_E_SHAPE)
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._k, self._v, self._k_scale, self._v_scale = k, v, k_scale, v_scale
         self._c = B.amap_cache(k.data_ptr(), v.data_ptr(), _ELEMENT[k.dtype], k.size(0), k.size(1), k.size(2), k.size(3), k.stride(0), k.stride(1), k.stride(2),
                                None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
+        self._cache_at = B.C.addressof(self._c)
+        self._work = {}   # cache_attend's workspace on each stream that it has been called on: one call after the other uses it there
+
+    # (the library has their addresses)
+    k, v, k_scale, v_scale = (property(operator.attrgetter(name)) for name in ("_k", "_v", "_k_scale", "_v_scale"))
 
     @property
     def page_size(self):
-        return self.k.size(1)
+        return self._k.size(1)
 
 
 class Assigned(NamedTuple):
@@ -198,10 +215,9 @@ class Assigned(NamedTuple):
 def assigned_buffers(requests, n_tokens, like=None) -> Assigned:
     """Room for a step's assignment, for a program that keeps it from step to step (as a captured graph has to)."""
     dev = require_gpu() if like is None else like.device
-    i32 = torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=dev)
-    slot = torch.empty(n_tokens, dtype=torch.int64, device=dev)
-    begin, length, taken, position, owner = torch.split(i32, (requests + 1, requests, 1, n_tokens, n_tokens))
-    return Assigned(begin, length, slot, position, owner, taken)
+    whole = torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=dev)
+    begin, length, taken, position, owner = whole.split_with_sizes((requests + 1, requests, 1, n_tokens, n_tokens))
+    return Assigned(begin, length, torch.empty(n_tokens, dtype=torch.int64, device=dev), position, owner, taken)
 
 
 def _made_on(stream):
@@ -216,6 +232,13 @@ def cache_assign(page_size, cached, fresh, table, free_pages, n_tokens, out=None
     """Pages, slots and positions for a step in which request r adds fresh[r] tokens to its cached[r] (None: none yet):
     new pages are taken from the head of free_pages into `table`, which is changed in place.  All int32."""
     what = "amap_cache_assign"
+    if stream is None and type(n_tokens) is int and n_tokens >= 0 and isinstance(fresh, torch.Tensor) and fresh.dim() == 1 and fresh.is_cuda:
+        if out is None:
+            out = assigned_buffers(fresh.size(0), n_tokens, fresh)
+        st = _assign(page_size, cached, fresh, table, free_pages, n_tokens, out, None)
+        if st >= 0:
+            B._check(st, what)
+            return out
     n = _on_gpu(fresh, torch.int32, 1, what, "fresh").size(0)
     _on_gpu(table, torch.int32, 2, what, "table")
     _on_gpu(free_pages, torch.int32, 1, what, "free_pages")
@@ -240,6 +263,12 @@ def rotary(x, rope, position, out=None, inverse=False, stream=None) -> torch.Ten
     """out = x [tokens, heads, head_dim] turned to its positions ([tokens] or [axes, tokens], int32); inverse: turned back, the
     gradient.  out may be x itself."""
     what = "amap_rotary"
+    if out is None and stream is None and isinstance(x, torch.Tensor) and x.is_cuda:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    st = _rotary(x, rope, position, out, inverse, stream)
+    if st >= 0:
+        B._check(st, what)
+        return out
     a = _rows(x, what, "x")
     if out is None:
         with _made_on(stream):
@@ -255,6 +284,12 @@ def cache_append(cache, k, v, slot, rope=None, position=None, q=None, q_out=None
     """k and v [tokens, kv_heads, head_dim] into the cache at slot [tokens] (int64; outside the cache: left out), k turned by the
     rope on the way, if there is one, and q into q_out (allocated if None; returned)."""
     what = "amap_cache_append"
+    if q is not None and q_out is None and stream is None and isinstance(q, torch.Tensor) and q.is_cuda:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    st = _append(cache, k, v, slot, rope, position, q, q_out, stream)
+    if st >= 0:
+        B._check(st, what)
+        return q_out
     a, b = _rows(k, what, "k"), _rows(v, what, "v")
     tokens, dim = k.size(0), cache.k.size(3)
     if v.size(0) != tokens or k.size(2) != dim or v.size(2) != dim or (q is not None and isinstance(q, torch.Tensor) and (q.size(0) != tokens or q.size(-1) != dim)):
@@ -280,12 +315,24 @@ def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=No
     `window` of them) that table [requests, width] (int32) leads to.  scale: 1 / sqrt(head_dim) if None.  A request that sees nothing has
     rows of 0 and lse -inf.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it."""
     what = "amap_cache_attend"
+    if stream is None and isinstance(q, torch.Tensor) and q.is_cuda and q.dim() == 3:
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if lse is None:
+            lse = q.new_empty((q.size(0), q.size(1)), dtype=torch.float32)
+        work = workspace
+        if work is None and not _capturing():
+            work = cache._work.get(current_stream())
+        st = _attend(cache, q, table, length, scale, window, out, lse, work, None)
+        if st >= 0:
+            B._check(st, what)
+            return out, lse
     a = _rows(q, what, "q")
     n, heads, dim = q.shape
     _on_gpu(table, torch.int32, 2, what, "table")
     if _on_gpu(length, torch.int32, 1, what, "length").size(0) != n or table.size(0) != n or dim != cache.k.size(3):
         raise _refused(what, "q, table, length and the cache differ in requests or head_dim", B.AMAP_E_SHAPE)
-    need = B.amap_cache_attend_workspace(cache._c, heads, n, table.size(1))
+    need = attend_workspace(cache, heads, n, table.size(1))
     with _made_on(stream):
         if out is None:
             out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
@@ -293,6 +340,8 @@ def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=No
             lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
         if workspace is None and need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            if stream is None and not _capturing():   # (a graph's memory is the graph's)
+                cache._work[current_stream()] = workspace
     if isinstance(out, torch.Tensor) and out.shape != q.shape:
         raise _refused(what, f"out is {tuple(out.shape)}, not {tuple(q.shape)}", B.AMAP_E_SHAPE)
     if _on_gpu(lse, torch.float32, 2, what, "lse").shape != (n, heads) or not lse.is_contiguous():
