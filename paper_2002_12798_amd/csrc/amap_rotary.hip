@@ -1,11 +1,11 @@
 // Rotary positions (amap_rotary) and the store of fresh keys and values through a slot map (amap_cache_append): rows of heads
 // read once, turned where there is something to turn, rounded once and written once.
 //
-// A workgroup takes a few tokens.  It first makes their angles, one pair per lane, in LDS, where every head finds them: the
-// angle is position x frequency in 64 bits, brought into one turn there (at position 100 000 a 32-bit product is off by 4e-3
-// of a radian), its sine and cosine in 32.  Then it goes over its units, the widest piece that the rows' layout allows
-// of one head of one tensor: both halves of the pairs, or a piece that holds whole pairs, or one that is only carried
-// over.  Bound by the bytes of the rows; the angles are a 64-bit multiplication or two per pair and token, for all heads.
+// A workgroup takes a few tokens.  A lane has one unit of a token's rows, the widest piece that their layout allows (both halves of the
+// pairs, or a piece that holds whole pairs, or one that is only carried over), and the same one of up to U tokens: what it
+// is and where it lies are worked out once.  Its loads are issued first; while they are on their way the workgroup makes the tokens' angles, one
+// pair per lane, in LDS, where every head finds them: the angle is position x frequency in 64 bits, brought into one turn
+// there (at position 100 000 a 32-bit product is off by 4e-3 of a radian), its sine and cosine in 32.  Bound by the bytes of the rows.
 #include "amap_cache.hpp"
 
 using namespace amap_cache_detail;
@@ -14,8 +14,8 @@ using namespace amap_dev;
 
 namespace {
 
-constexpr int kTurnThreads = 256, kMaxJobs = 3, kUnitsAtOnce = 4;
-constexpr uint32_t kAnglesAtOnce = 2048;   // 16 KB of them
+constexpr int kMostThreads = 512, kMaxJobs = 3, kAtOnce = 4;   // tokens of a lane
+constexpr uint32_t kMostAngles = 4096;   // 32 KB of them
 constexpr int kMaxDim = 2048;
 
 // one tensor's way: where it comes from, where it goes
@@ -35,12 +35,13 @@ struct TurnArgs {
     const int32_t *position;
     const int64_t *slot;
     int64_t axis_stride, n_slots;
-    uint32_t tokens, dim, pairs, interleaved, n_jobs, inverse;
+    uint32_t tokens, pairs, interleaved, n_jobs, inverse, page;
     uint32_t axis_end[AMAP_MAX_AXES];
-    uint32_t page;
-    uint32_t group, splits;    // tokens of a workgroup; workgroups that share them
     uint32_t units;            // of one token, all jobs
-    FastDiv by_token, by_split, by_pairs;
+    uint32_t width, beside;    // lanes to one token, tokens side by side
+    uint32_t each, group;      // tokens of a lane, of a workgroup
+    uint32_t rounds, splits;   // rounds of `width` units to all of a token's, dealt to so many workgroups
+    FastDiv by_width, by_split, by_pairs;
 };
 
 template <int BYTES>
@@ -87,25 +88,39 @@ __device__ __forceinline__ float widen<F16>(const char *at) {
     return (float)x;
 }
 
+// x / s, by whose reciprocal: rounded as the division is but for some last places (one correction of the product; a quotient that is
+// not finite has none)
+__device__ __forceinline__ float over(float x, float s, float reciprocal) {
+    const float q = x * reciprocal, r = __builtin_fmaf(-q, s, x);
+    return __builtin_isfinite(q) ? __builtin_fmaf(r, reciprocal, q) : q;
+}
+
+template <bool STREAM, class P>
+__device__ __forceinline__ void put(char *at, P p) {
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(p, reinterpret_cast<P *>(at));
+    else
+        *reinterpret_cast<P *>(at) = p;
+}
 // V values rounded to nearest even and stored in one access
-template <int V>
+template <int V, bool STREAM>
 __device__ __forceinline__ void store_as(uint32_t type, char *at, const float (&x)[V]) {
     if (type == AMAP_F32) {
         if constexpr (V * 4 <= 16) {
             typename Piece<V * 4>::type p;
             __builtin_memcpy(&p, x, sizeof(p));
-            *reinterpret_cast<typename Piece<V * 4>::type *>(at) = p;
+            put<STREAM>(at, p);
         }
     } else if (type == AMAP_E4M3) {
-        uint8_t b[V];
+        float y[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float y = x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.f), 448.f);
-            b[i] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false);
-        }
+        for (int i = 0; i < V; ++i) y[i] = x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.f), 448.f);
+        uint16_t b[V > 1 ? V / 2 : 1];
+#pragma unroll
+        for (int i = 0; i < (V > 1 ? V / 2 : 1); ++i) b[i] = (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2 * i], y[V > 1 ? 2 * i + 1 : 0], 0, false);
         typename Piece<V>::type p;
         __builtin_memcpy(&p, b, V);
-        *reinterpret_cast<typename Piece<V>::type *>(at) = p;
+        put<STREAM>(at, p);
     } else {
         uint16_t h[V];
 #pragma unroll
@@ -113,109 +128,107 @@ __device__ __forceinline__ void store_as(uint32_t type, char *at, const float (&
             h[i] = type == AMAP_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)x[i]) : __builtin_bit_cast(uint16_t, (_Float16)x[i]);
         typename Piece<V * 2>::type p;
         __builtin_memcpy(&p, h, sizeof(p));
-        *reinterpret_cast<typename Piece<V * 2>::type *>(at) = p;
+        put<STREAM>(at, p);
     }
 }
 
-// T: the rows' type; BYTES: of one access to them
-template <class T, int BYTES>
-__global__ __launch_bounds__(kTurnThreads) void amap_turn_kernel(const TurnArgs a) {
-    constexpr int V = BYTES / T::bytes;
+// T: the rows' type; BYTES: of one access to them; HALVES: a pair's elements in two accesses; STREAM: stores past the caches
+template <class T, int BYTES, bool HALVES, bool STREAM>
+__global__ __launch_bounds__(kMostThreads) void amap_turn_kernel(const TurnArgs a) {
+    constexpr int V = BYTES / T::bytes, U = kAtOnce;
     typedef typename Piece<BYTES>::type piece;
     extern __shared__ char lds[];
-    float2 *const angle = reinterpret_cast<float2 *>(lds);   // [group][pairs]: cosine, sine
-    const uint32_t tid = threadIdx.x;
-    const uint32_t block = fdiv(blockIdx.x, a.by_split), split = blockIdx.x - block * a.splits;
+    int64_t *const place = reinterpret_cast<int64_t *>(lds);                          // [group]: of a token's row in the cache, -1: none
+    float2 *const angle = reinterpret_cast<float2 *>(lds + 8u * (a.slot ? a.group : 0u));   // [group][pairs]: cosine, sine
+    const uint32_t tid = threadIdx.x, block = fdiv(blockIdx.x, a.by_split), split = blockIdx.x - block * a.splits;
     const uint32_t t0 = block * a.group, count = min(a.group, a.tokens - t0);
-    for (uint32_t i = tid; i < count * a.pairs; i += kTurnThreads) {
-        const uint32_t t = fdiv(i, a.by_pairs), p = i - t * a.pairs;
-        uint32_t axis = 0;
+    const uint32_t beside = fdiv(tid, a.by_width), in = tid - beside * a.width;
+    for (uint32_t round = split; round < a.rounds; round += a.splits) {
+        // ---- this lane's unit
+        uint32_t u = round * a.width + in, j = 0;
+        const bool mine = u < a.units && beside < a.beside;
+        if (!mine) u = 0;
+        while (j + 1 < a.n_jobs && u >= a.job[j].units) u -= a.job[j++].units;
+        const TurnJob &job = a.job[j];
+        const uint32_t head = fdiv(u, job.by_head);
+        u -= head * job.per_head;
+        const uint32_t halves = HALVES && job.turns ? a.pairs / V : 0u;
+        const bool turned = HALVES ? u < halves : job.turns && u * V < 2u * a.pairs;
+        const uint32_t at = u < halves ? u * V : (u + halves) * V;   // its first element: of the first halves, or of what lies behind both
+        const char *const src = job.src + ((int64_t)(t0 + beside) * job.src_token + (int64_t)head * job.src_head + at) * T::bytes;
+        const int64_t step = (int64_t)a.beside * job.src_token * T::bytes;
+        piece x[U], y[U];
 #pragma unroll
-        for (int k = 0; k + 1 < AMAP_MAX_AXES; ++k) axis += p >= a.axis_end[k];
-        const double turns = (double)a.position[axis * a.axis_stride + t0 + t] * (double)a.freq[p] * 0.15915494309189533577;   // 1 / (2 pi)
-        float s, c;
-        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-        angle[i] = make_float2(c, a.inverse ? -s : s);
-    }
-    if (a.pairs) __syncthreads();
-    const uint32_t total = count * a.units;
-    for (uint32_t base = split * kTurnThreads * kUnitsAtOnce; base < total; base += a.splits * kTurnThreads * kUnitsAtOnce) {
-        piece x[kUnitsAtOnce], y[kUnitsAtOnce];
-        char *dst[kUnitsAtOnce];
-        uint32_t at[kUnitsAtOnce], turned[kUnitsAtOnce], type[kUnitsAtOnce];   // turned: 0 carried over, 1 halves, 2 neighbours
-        float scale[kUnitsAtOnce];
-        uint32_t tok[kUnitsAtOnce];
-#pragma unroll
-        for (int k = 0; k < kUnitsAtOnce; ++k) {
-            const uint32_t i = base + k * kTurnThreads + tid;
-            dst[k] = nullptr;
-            if (i >= total) continue;
-            const uint32_t t = fdiv(i, a.by_token);
-            uint32_t u = i - t * a.units, j = 0;
-            while (j + 1 < a.n_jobs && u >= a.job[j].units) u -= a.job[j++].units;
-            const TurnJob &job = a.job[j];
-            const uint32_t head = fdiv(u, job.by_head);
-            u -= head * job.per_head;
-            const uint32_t halves = job.turns && !a.interleaved ? a.pairs / V : 0u;
-            // the unit's first element: of the first halves, then of what lies behind both
-            at[k] = u < halves ? u * V : (u + halves) * V;
-            turned[k] = u < halves ? 1u : job.turns && a.interleaved && at[k] < 2u * a.pairs ? 2u : 0u;
-            tok[k] = t;
-            type[k] = job.out_type;
-            scale[k] = job.scale ? job.scale[head] : 1.f;
-            const char *src = job.src + ((int64_t)(t0 + t) * job.src_token + (int64_t)head * job.src_head + at[k]) * T::bytes;
-            int64_t to = (int64_t)head * job.dst_head + at[k];
-            if (job.to_cache) {
-                const int64_t slot = a.slot[t0 + t];
-                if (slot < 0 || slot >= a.n_slots) continue;
-                const int64_t page = slot / a.page;
-                to += page * job.dst_page + (slot - page * a.page) * job.dst_token;
-            } else {
-                to += (int64_t)(t0 + t) * job.dst_token;
-            }
-            x[k] = *reinterpret_cast<const piece *>(src);
-            if (turned[k] == 1u) y[k] = *reinterpret_cast<const piece *>(src + (size_t)a.pairs * T::bytes);
-            const uint32_t es = type[k] == AMAP_F32 ? 4u : type[k] == AMAP_E4M3 ? 1u : 2u;
-            dst[k] = job.dst + to * es;
+        for (int k = 0; k < U; ++k) {
+            if (!mine || (uint32_t)k >= a.each || beside + k * a.beside >= count) continue;
+            x[k] = *reinterpret_cast<const piece *>(src + k * step);
+            if (HALVES && turned) y[k] = *reinterpret_cast<const piece *>(src + k * step + (size_t)a.pairs * T::bytes);
         }
-#pragma unroll
-        for (int k = 0; k < kUnitsAtOnce; ++k) {
-            if (!dst[k]) continue;
-            float u[V], w[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) u[v] = widen<T>(reinterpret_cast<const char *>(&x[k]) + v * T::bytes);
-            const float2 *const cs = angle + tok[k] * a.pairs;
-            if (turned[k] == 1u) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float b = widen<T>(reinterpret_cast<const char *>(&y[k]) + v * T::bytes), f = u[v];
-                    const float2 t = cs[at[k] + v];
-                    u[v] = f * t.x - b * t.y;
-                    w[v] = b * t.x + f * t.y;
+        if (round == split) {
+            if (a.slot)
+                for (uint32_t i = tid; i < count; i += blockDim.x) {
+                    const int64_t slot = a.slot[t0 + i], page = slot / a.page;   // (the caches' strides are the first job's)
+                    place[i] = slot >= 0 && slot < a.n_slots ? page * a.job[0].dst_page + (slot - page * a.page) * a.job[0].dst_token : -1;
                 }
-                if (scale[k] != 1.f) {
+            for (uint32_t i = tid; i < count * a.pairs; i += blockDim.x) {
+                const uint32_t t = fdiv(i, a.by_pairs), p = i - t * a.pairs;
+                uint32_t axis = 0;
 #pragma unroll
-                    for (int v = 0; v < V; ++v) w[v] /= scale[k];
+                for (int k = 0; k + 1 < AMAP_MAX_AXES; ++k) axis += p >= a.axis_end[k];
+                const double turns = (double)a.position[axis * a.axis_stride + t0 + t] * (double)a.freq[p] * 0.15915494309189533577;   // 1 / (2 pi)
+                float s, c;
+                sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+                angle[i] = make_float2(c, a.inverse ? -s : s);
+            }
+            __syncthreads();
+        }
+        const uint32_t type = job.out_type, es = type == AMAP_F32 ? 4u : type == AMAP_E4M3 ? 1u : 2u;
+        const float scale = job.scale ? job.scale[head] : 1.f, reciprocal = 1.f / scale;
+        const int64_t in_token = (int64_t)head * job.dst_head + at;
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const uint32_t t = beside + k * a.beside;
+            if (!mine || (uint32_t)k >= a.each || t >= count) continue;
+            const int64_t to = job.to_cache ? place[t] : (int64_t)(t0 + t) * job.dst_token;
+            if (to < 0) continue;
+            char *const dst = job.dst + (to + in_token) * es;
+            float v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = widen<T>(reinterpret_cast<const char *>(&x[k]) + e * T::bytes);
+            const float2 *const cs = angle + t * a.pairs;
+            if constexpr (HALVES) {
+                if (turned) {
+                    float w[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float b = widen<T>(reinterpret_cast<const char *>(&y[k]) + e * T::bytes), f = v[e];
+                        const float2 c = cs[at + e];
+                        v[e] = f * c.x - b * c.y;
+                        w[e] = b * c.x + f * c.y;
+                    }
+                    if (scale != 1.f) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) w[e] = over(w[e], scale, reciprocal);
+                    }
+                    store_as<V, STREAM>(type, dst + a.pairs * es, w);
                 }
-                const uint32_t es = type[k] == AMAP_F32 ? 4u : type[k] == AMAP_E4M3 ? 1u : 2u;
-                store_as<V>(type[k], dst[k] + a.pairs * es, w);
-            } else if (turned[k] == 2u) {
-                if constexpr (V > 1) {
+            } else if constexpr (V > 1) {
+                if (turned) {
 #pragma unroll
-                    for (int v = 0; v < V; v += 2)
-                        if (at[k] + v < 2u * a.pairs) {
-                            const float f = u[v], b = u[v + 1];
-                            const float2 t = cs[(at[k] + v) >> 1];
-                            u[v] = f * t.x - b * t.y;
-                            u[v + 1] = b * t.x + f * t.y;
+                    for (int e = 0; e < V; e += 2)
+                        if (at + e < 2u * a.pairs) {
+                            const float f = v[e], b = v[e + 1];
+                            const float2 c = cs[(at + e) >> 1];
+                            v[e] = f * c.x - b * c.y;
+                            v[e + 1] = b * c.x + f * c.y;
                         }
                 }
             }
-            if (scale[k] != 1.f) {
+            if (scale != 1.f) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) u[v] /= scale[k];
+                for (int e = 0; e < V; ++e) v[e] = over(v[e], scale, reciprocal);
             }
-            store_as<V>(type[k], dst[k], u);
+            store_as<V, STREAM>(type, dst, v);
         }
     }
 }
@@ -243,16 +256,28 @@ struct Way {
     const float *scale;
 };
 
-template <class T, int BYTES>
-hipError_t turn(const TurnArgs &g, uint32_t grid, uint32_t lds, hipStream_t s) {
-    return launch_kernel<amap_turn_kernel<T, BYTES>>(dim3(grid), dim3(kTurnThreads), lds, s, g);
+template <class T, int BYTES, bool STREAM>
+hipError_t turn(bool halves, const TurnArgs &g, uint32_t grid, uint32_t threads, uint32_t lds, hipStream_t s) {
+    return halves ? launch_kernel<amap_turn_kernel<T, BYTES, true, STREAM>>(dim3(grid), dim3(threads), lds, s, g)
+                  : launch_kernel<amap_turn_kernel<T, BYTES, false, STREAM>>(dim3(grid), dim3(threads), lds, s, g);
 }
 template <class T>
-hipError_t turn_by(int bytes, const TurnArgs &g, uint32_t grid, uint32_t lds, hipStream_t s) {
-    if (bytes == 16) return turn<T, 16>(g, grid, lds, s);
-    if (bytes == 8) return turn<T, 8>(g, grid, lds, s);
-    if (T::bytes == 2 && bytes == 2) return turn<T, T::bytes>(g, grid, lds, s);
-    return turn<T, 4>(g, grid, lds, s);
+hipError_t turn_by(int bytes, bool halves, bool stream, const TurnArgs &g, uint32_t grid, uint32_t threads, uint32_t lds, hipStream_t s) {
+    if (bytes == 16) return stream ? turn<T, 16, true>(halves, g, grid, threads, lds, s) : turn<T, 16, false>(halves, g, grid, threads, lds, s);
+    if (bytes == 8) return turn<T, 8, false>(halves, g, grid, threads, lds, s);
+    if (T::bytes == 2 && bytes == 2) return turn<T, T::bytes, false>(halves, g, grid, threads, lds, s);
+    return turn<T, 4, false>(halves, g, grid, threads, lds, s);
+}
+
+// Threads of a workgroup for rows of so many units: as few lanes as possible without one (64 .. 512 in steps of 64; 256 where others are no better).
+uint32_t threads_for(uint64_t units) {
+    uint32_t best = 256;
+    double most = 0.0;
+    for (uint32_t n : {256u, 320u, 384u, 448u, 512u, 192u, 128u}) {
+        const double held = units <= n ? (double)(n / units * units) / n : (double)units / (double)((units + n - 1) / n * n);
+        if (held > most + 0.03) most = held, best = n;
+    }
+    return best;
 }
 
 amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope *rope, const int32_t *position, int64_t axis_stride, int inverse, const int64_t *slot,
@@ -281,7 +306,6 @@ amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope 
     TurnArgs g = {};
     g.n_jobs = (uint32_t)n;
     g.tokens = (uint32_t)tokens;
-    g.dim = (uint32_t)dim;
     if (rope) {
         g.freq = rope->freq;
         g.position = position;
@@ -323,28 +347,44 @@ amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope 
     }
     if (units > (1u << 24)) return refuse("more than 2^24 pieces in the rows of one token");
     g.units = (uint32_t)units;
-    g.by_token = make_fastdiv(g.units);
     g.by_pairs = make_fastdiv(g.pairs ? g.pairs : 1u);
-    // tokens of a workgroup: two passes over its units, as far as their angles find room
-    const uint32_t pass = kTurnThreads * kUnitsAtOnce;
-    uint64_t group = 2 * pass / units;
-    if (g.pairs && group > kAnglesAtOnce / g.pairs) group = kAnglesAtOnce / g.pairs;
-    if (group < 1) group = 1;
-    // few tokens: fewer of them each, down to one, and several workgroups to one token
-    while (group > 1 && (uint64_t)tokens < 512 * group) group = (group + 1) / 2;
-    const uint64_t blocks = ((uint64_t)tokens + group - 1) / group, passes = (group * units + pass - 1) / pass;
-    uint64_t splits = blocks >= 512 ? 1 : passes;
-    if (blocks * splits >= (1u << 31)) return refuse("too many tokens for one launch");
-    g.group = (uint32_t)group;
-    g.splits = (uint32_t)splits;
+    uint32_t threads = threads_for(units);
+    g.width = units < threads ? (uint32_t)units : threads;
+    g.beside = threads / g.width;
+    g.by_width = make_fastdiv(g.width);
+    if (g.pairs && g.beside > kMostAngles / g.pairs) g.beside = kMostAngles / g.pairs;   // (pairs <= 1024: at least 4)
+    // tokens of a lane: as many as it loads at once, while that leaves every compute unit two workgroups
+    g.each = kAtOnce;
+    if (g.pairs && g.each * g.beside > kMostAngles / g.pairs) g.each = kMostAngles / g.pairs / g.beside;
+    while (g.each > 1 && (uint64_t)tokens < 512ull * g.beside * g.each) g.each /= 2;
+    while (g.beside > 1 && (uint64_t)tokens < 512ull * g.beside) g.beside = (g.beside + 1) / 2;
+    g.group = g.beside * g.each;
+    threads = (g.width * g.beside + 63u) / 64u * 64u;
+    g.rounds = (g.units + g.width - 1) / g.width;
+    const uint64_t blocks = ((uint64_t)tokens + g.group - 1) / g.group;
+    g.splits = blocks >= 512 ? 1 : g.rounds;
+    if (blocks * g.splits >= (1u << 31)) return refuse("too many tokens for one launch");
     g.by_split = make_fastdiv(g.splits);
-    const uint32_t lds = g.group * g.pairs * 8u, grid = (uint32_t)(blocks * splits);
+    const uint32_t lds = g.group * g.pairs * 8u + (slot ? 8u * g.group : 0u), grid = (uint32_t)(blocks * g.splits);
     const StreamDevice device(s);
     if (device.status() != hipSuccess) return launched(device.status(), "the stream's device");
     const int bytes = (int)width * es;
-    const hipError_t e = type == AMAP_F32    ? turn_by<F32>(bytes, g, grid, lds, s)
-                         : type == AMAP_BF16 ? turn_by<Bf16>(bytes, g, grid, lds, s)
-                                             : turn_by<F16>(bytes, g, grid, lds, s);
+    // Past the caches where every run of a store is whole 64-byte pieces at both ends: [65536,16,128] bf16 106 -> 98 us, [16391,8,128] k and v stored
+    // 34 -> 25, but rows of 160 bytes in two halves of 80 20.4 -> 24.
+    const bool paired = rope && !rope->interleaved;
+    uint64_t runs = 0;
+    for (int i = 0; i < n; ++i) {
+        const Way &w = way[i];
+        const uint64_t out = (uint64_t)bytes_of(w.out);
+        // (heads that follow one another are one run, unless their halves are stored apart)
+        const bool apart = paired && w.turns, joined = !apart && w.head == dim;
+        runs |= reinterpret_cast<uintptr_t>(w.dst) | out * ((uint64_t)w.token | (uint64_t)w.page);
+        runs |= out * (joined ? (uint64_t)dim * (uint64_t)w.in->heads : (uint64_t)w.head | (uint64_t)dim | (apart ? (uint64_t)rope->pairs : 0u));
+    }
+    const bool past = runs % 64 == 0;
+    const hipError_t e = type == AMAP_F32    ? turn_by<F32>(bytes, paired, past, g, grid, threads, lds, s)
+                         : type == AMAP_BF16 ? turn_by<Bf16>(bytes, paired, past, g, grid, threads, lds, s)
+                                             : turn_by<F16>(bytes, paired, past, g, grid, threads, lds, s);
     return launched(e, "amap_turn_kernel");
 }
 
