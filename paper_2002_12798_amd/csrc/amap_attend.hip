@@ -30,7 +30,6 @@ constexpr int kTokens = 32;        // of a wavefront's step
 constexpr int kColumns = 16;       // queries of a workgroup at a time (8 where their weights' second parts have the others)
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 constexpr uint32_t kBegin = 3;             // what beginning and ending a segment counts for in a share, in tiles
-constexpr uint32_t kFewSegments = 128;     // up to so many are joined row by row: they are in many pieces each
 constexpr uint32_t kMostJoining = 4096;    // workgroups of a join
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
@@ -151,25 +150,38 @@ __device__ __forceinline__ void landed() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
 }
 // N loads of 16 bytes a lane, 1 KB apart in LDS: load i from base + off[i] (off counts 4096 - 1024 (i % 4) on top: the instruction's offset counts on both
-// sides, so that one write of M0 serves four; base is 4096 less).  The first half of them from `lo`, the others from `hi`.
-template <int N>
+// sides, so that one write of M0 serves four; base is 4096 less).  The first half of them from `lo`, the others from `hi`.  Past the caches where no
+// other workgroup reads the same (ONCE): 205 -> 183 us over 1.07 GB; with four workgroups to a key head 30 -> 38.
+#define AMAP_ROWS_OF_FOUR(HINT)                                                                                                                          \
+    asm volatile("s_mov_b32 m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4" HINT "\n\tglobal_load_lds_dwordx4 %1, %5 offset:1024" HINT "\n\t"         \
+                 "global_load_lds_dwordx4 %2, %6 offset:2048" HINT "\n\tglobal_load_lds_dwordx4 %3, %7 offset:3072" HINT ::"v"(off[i]),                    \
+                 "v"(off[i + 1 < N ? i + 1 : 0]), "v"(off[i + 2 < N ? i + 2 : 0]), "v"(off[i + 3 < N ? i + 3 : 0]), "s"(b0), "s"(b1), "s"(b2), "s"(b3), "s"(at)       \
+                 : "memory")
+#define AMAP_ROWS_OF_TWO(HINT)                                                                                                                            \
+    asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" HINT "\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024" HINT ::"v"(off[i]), \
+                 "v"(off[i + 1 < N ? i + 1 : 0]), "s"(b0), "s"(b1), "s"(at)                                                                                  \
+                 : "memory")
+template <bool ONCE, int N>
 __device__ __forceinline__ void load_rows(const char *lo, const char *hi, const uint32_t (&off)[N], uint32_t lds) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
         const uint32_t at = lds + 1024u * i;
         const char *const b0 = 2 * i < N ? lo : hi, *const b1 = 2 * i + 2 < N ? lo : hi, *const b2 = 2 * i + 4 < N ? lo : hi, *const b3 = 2 * i + 6 < N ? lo : hi;
-        if (i + 4 <= N)
-            asm volatile(
-                "s_mov_b32 m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %5 offset:1024\n\t"
-                "global_load_lds_dwordx4 %2, %6 offset:2048\n\tglobal_load_lds_dwordx4 %3, %7 offset:3072" ::"v"(off[i]),
-                "v"(off[i + 1 < N ? i + 1 : 0]), "v"(off[i + 2 < N ? i + 2 : 0]), "v"(off[i + 3 < N ? i + 3 : 0]), "s"(b0), "s"(b1), "s"(b2), "s"(b3), "s"(at)
-                : "memory");
-        else
-            asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %3 offset:1024" ::"v"(off[i]),
-                         "v"(off[i + 1 < N ? i + 1 : 0]), "s"(b0), "s"(b1), "s"(at)
-                         : "memory");
+        if constexpr (ONCE) {
+            if (i + 4 <= N)
+                AMAP_ROWS_OF_FOUR(" nt");
+            else
+                AMAP_ROWS_OF_TWO(" nt");
+        } else {
+            if (i + 4 <= N)
+                AMAP_ROWS_OF_FOUR("");
+            else
+                AMAP_ROWS_OF_TWO("");
+        }
     }
 }
+#undef AMAP_ROWS_OF_FOUR
+#undef AMAP_ROWS_OF_TWO
 // the larger (sum) of what the four lanes of one column hold
 __device__ __forceinline__ float top_of_column(float x) {
     const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -319,7 +331,10 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
         const char *const zeros = reinterpret_cast<const char *>(&kZeros);
         auto load_side = [&](const char *from, const uint32_t (&off)[F::LOADS], const uint32_t (&piece)[F::LOADS], uint32_t lds) __attribute__((always_inline)) {
             if (fast) {
-                load_rows<F::LOADS>(from + lo, from + hi, off, lds);
+                if (F::PAIRED || a.blocks == 1)
+                    load_rows<true>(from + lo, from + hi, off, lds);
+                else
+                    load_rows<false>(from + lo, from + hi, off, lds);
             } else {
                 uint32_t x[F::LOADS];
 #pragma unroll
@@ -524,15 +539,15 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
 
 // The segments that were cut, their pieces joined: a segment (all its rows at once) or one row of it to a workgroup.
 struct JoinArgs {
-    const float *parts;
+    const float *parts_at;
     const Split *splits;
     char *out;
     float *lse;
     const float *v_scale;
     int64_t out_token, out_head;
-    uint32_t work, rows, columns, group, heads, dim;   // rows: row blocks of a segment, 1 or `columns`
-    FastDiv by_rows, by_segments, by_blocks;
-    uint32_t segments, blocks;
+    uint32_t work, at_once, columns, group, heads, dim;   // at_once: rows of a workgroup
+    FastDiv by_parts, by_segments, by_blocks;             // parts: workgroups to a segment
+    uint32_t parts, segments, blocks;
 };
 
 template <class T, int DP>
@@ -542,56 +557,53 @@ __global__ __launch_bounds__(256) void amap_attend_join_kernel(const JoinArgs a)
     __shared__ f32x4 results[kSlots][kLanes];
     const uint32_t slot = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, d = 4u * lane;
     for (uint32_t i = blockIdx.x; i < a.work; i += gridDim.x) {
-        const uint32_t id = fdiv(i, a.by_rows), row_block = i - id * a.rows;
+        const uint32_t id = fdiv(i, a.by_parts), c0 = (i - id * a.parts) * a.at_once;
         const Split s = a.splits[id];
         if (s.count == 0) continue;
         const uint32_t r = fdiv(id, a.by_segments), segment = id - r * a.segments;
         const uint32_t kv = fdiv(segment, a.by_blocks), block = segment - kv * a.blocks, rows = min(a.group - block * a.columns, a.columns);
-        // a slot has one row of so many at once, and every so-manieth piece of it
-        const uint32_t at_once = a.rows > 1 ? 1u : min(rows, kSlots), ways = kSlots / at_once, way = slot / at_once;
-        const float *const first = a.parts + (size_t)(2u * s.group) * kPart;
-        for (uint32_t c0 = row_block; c0 < (a.rows > 1 ? min(row_block + 1, rows) : rows); c0 += at_once) {
-            const uint32_t c = c0 + slot % at_once;
-            float high = -INFINITY, sum = 0.f;
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
-            if (way < ways && c < rows) {
+        // a slot has one row of so many, and every so-manieth piece of it
+        const uint32_t ways = kSlots / a.at_once, way = slot / a.at_once, c = c0 + slot % a.at_once;
+        const float *const first = a.parts_at + (size_t)(2u * s.group) * kPart;
+        float high = -INFINITY, sum = 0.f;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (way < ways && c < rows) {
 #pragma unroll 4
-                for (uint32_t p = way; p < s.count; p += ways) {
-                    const float *const part = first + (size_t)(p ? 2u * p : 1u) * kPart;
-                    const float m = part[c], l = part[kColumns + c];
-                    const f32x4 y = *reinterpret_cast<const f32x4 *>(part + 2 * kColumns + c * DP + d);
-                    const float up = fmaxf(high, m), base = up == -INFINITY ? 0.f : up;
-                    const float keep = __builtin_amdgcn_exp2f(high - base), take = __builtin_amdgcn_exp2f(m - base);
-                    sum = sum * keep + l * take;
-                    x = x * keep + y * take;
-                    high = up;
-                }
+            for (uint32_t p = way; p < s.count; p += ways) {
+                const float *const part = first + (size_t)(p ? 2u * p : 1u) * kPart;
+                const float m = part[c], l = part[kColumns + c];
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(part + 2 * kColumns + c * DP + d);
+                const float up = fmaxf(high, m), base = up == -INFINITY ? 0.f : up;
+                const float keep = __builtin_amdgcn_exp2f(high - base), take = __builtin_amdgcn_exp2f(m - base);
+                sum = sum * keep + l * take;
+                x = x * keep + y * take;
+                high = up;
             }
-            if (slot < kSlots) {
-                results[slot][lane] = x;
-                if (lane == 0) tops[slot] = high, sums[slot] = sum;
-            }
-            __syncthreads();
-            if (way == 0 && c < rows) {
-                for (uint32_t w = 1; w < ways; ++w) {
-                    const uint32_t other = slot + w * at_once;
-                    const float m = tops[other], up = fmaxf(high, m), base = up == -INFINITY ? 0.f : up;
-                    const float keep = __builtin_amdgcn_exp2f(high - base), take = __builtin_amdgcn_exp2f(m - base);
-                    sum = sum * keep + sums[other] * take;
-                    x = x * keep + results[other][lane] * take;
-                    high = up;
-                }
-                const bool none = sum == 0.f;
-                const uint32_t h = kv * a.group + block * a.columns + c;
-                const float by = none ? 0.f : (a.v_scale ? a.v_scale[kv] : 1.f) / sum;
-                typename Of<T>::one *const out = reinterpret_cast<typename Of<T>::one *>(a.out) + (int64_t)r * a.out_token + (int64_t)h * a.out_head;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (d + e < a.dim) out[d + e] = (typename Of<T>::one)(none ? 0.f : x[e] * by);
-                if (lane == 0 && a.lse) a.lse[(int64_t)r * a.heads + h] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
-            }
-            __syncthreads();
         }
+        if (slot < kSlots) {
+            results[slot][lane] = x;
+            if (lane == 0) tops[slot] = high, sums[slot] = sum;
+        }
+        __syncthreads();
+        if (way == 0 && c < rows) {
+            for (uint32_t w = 1; w < ways; ++w) {
+                const uint32_t other = slot + w * a.at_once;
+                const float m = tops[other], up = fmaxf(high, m), base = up == -INFINITY ? 0.f : up;
+                const float keep = __builtin_amdgcn_exp2f(high - base), take = __builtin_amdgcn_exp2f(m - base);
+                sum = sum * keep + sums[other] * take;
+                x = x * keep + results[other][lane] * take;
+                high = up;
+            }
+            const bool none = sum == 0.f;
+            const uint32_t h = kv * a.group + block * a.columns + c;
+            const float by = none ? 0.f : (a.v_scale ? a.v_scale[kv] : 1.f) / sum;
+            typename Of<T>::one *const out = reinterpret_cast<typename Of<T>::one *>(a.out) + (int64_t)r * a.out_token + (int64_t)h * a.out_head;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (d + e < a.dim) out[d + e] = (typename Of<T>::one)(none ? 0.f : x[e] * by);
+            if (lane == 0 && a.lse) a.lse[(int64_t)r * a.heads + h] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+        __syncthreads();
     }
 }
 
@@ -612,9 +624,13 @@ amap_status attend(AttendArgs a, const Cut &cut, hipStream_t s) {
     }
     hipError_t e = launch_kernel<amap_attend_kernel<F>>(dim3(cut.groups), dim3(64), F::LDS, s, a);
     if (e != hipSuccess || !cut.splits) return launched(e, "amap_attend_kernel");
-    const uint32_t segments = a.requests * a.segments, rows = segments <= kFewSegments ? a.columns : 1u, work = segments * rows;
-    const JoinArgs j{a.parts, a.splits, a.out, a.lse, a.v_scale, a.out_token, a.out_head, work, rows, a.columns, a.group, a.heads, a.dim, make_fastdiv(rows), a.by_segments, a.by_blocks,
-                     a.segments, a.blocks};
+    // as many lanes to a row as there are pieces of a segment, if all are split alike
+    const uint32_t segments = a.requests * a.segments, rows = a.columns < a.group ? a.columns : a.group, slots = 256u / (F::DP / 4), pieces = 1u + cut.groups / segments;
+    uint32_t at_once = slots / pieces;
+    at_once = at_once < 1 ? 1 : at_once > rows ? rows : at_once;
+    const uint32_t parts = (rows + at_once - 1) / at_once, work = segments * parts;
+    const JoinArgs j{a.parts, a.splits, a.out, a.lse, a.v_scale, a.out_token, a.out_head, work, at_once, a.columns, a.group, a.heads, a.dim, make_fastdiv(parts), a.by_segments, a.by_blocks,
+                     parts, a.segments, a.blocks};
     e = launch_kernel<amap_attend_join_kernel<typename F::T, F::DP>>(dim3(work < kMostJoining ? work : kMostJoining), dim3(256), 0, s, j);
     return launched(e, "amap_attend_join_kernel");
 }

@@ -13,7 +13,7 @@ using namespace amap_dev;
 
 namespace {
 
-constexpr int kAssignThreads = 512, kAssignWaves = kAssignThreads / 64, kTokensPerThread = 4;
+constexpr int kAssignThreads = 512, kAssignWaves = kAssignThreads / 64;
 constexpr int64_t kMaxRequests = 16384;   // two sums each in 128 KB of LDS
 
 struct AssignArgs {
@@ -148,8 +148,7 @@ extern "C" amap_status amap_cache_assign(const amap_assign *a, void *stream) {
     }
     const AssignArgs g{a->cached, a->fresh, a->free_pages, a->table, a->begin, a->length, a->position, a->owner, a->taken, a->slot, a->table_stride, a->n_tokens,
                        a->n_free, (uint32_t)a->requests, (uint32_t)a->page_size, a->table_width};
-    constexpr int64_t kShare = kAssignThreads * kTokensPerThread;
-    const int64_t most = 1024, wanted = (a->n_tokens + kShare - 1) / kShare;
+    const int64_t most = 1024, wanted = (a->n_tokens + kAssignThreads - 1) / kAssignThreads;   // (what the chip holds at once)
     const uint32_t grid = (uint32_t)(wanted < 1 ? 1 : wanted > most ? most : wanted);
     return launched(launch_kernel<amap_assign_kernel>(dim3(grid), dim3(kAssignThreads), lds, s, g), "amap_assign_kernel");
 }

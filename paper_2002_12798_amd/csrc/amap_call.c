@@ -413,7 +413,8 @@ static PyObject *call_attend(PyObject *self, PyObject *const *a, Py_ssize_t n)
     CALLED(p_attend(cache, &q, tq.size[0], tt.data, tt.stride[0], (int)tt.size[1], tl.data, (float)scale, (int)window, &out, te.data, tw.data, tw.size[0], stream));
 }
 
-/* assign(page size, cached or None, fresh, table, free pages, n_tokens, (begin, length, slot, position, owner, taken), stream or None) */
+/* assign(page size, cached or None, fresh, table, free pages, n_tokens, outputs, stream or None).  Outputs: begin, length, slot, position, owner, taken; or the
+ * two buffers they are all parts of, int32 with begin, length, taken, position and owner one after the other, and int64 for the slots. */
 static PyObject *call_assign(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     tensor_t tc, tf, tt, tp, out[6];
@@ -424,10 +425,19 @@ static PyObject *call_assign(PyObject *self, PyObject *const *a, Py_ssize_t n)
     UNLESS(p_assign && n == 8 && of_type(a[2], 1, t_int32, &tf) && of_type(a[3], 2, t_int32, &tt) && of_type(a[4], 1, t_int32, &tp) && tt.size[0] == tf.size[0]);
     tc.data = NULL;
     if (a[1] != Py_None) UNLESS(of_type(a[1], 1, t_int32, &tc) && tc.size[0] == tf.size[0]);
-    UNLESS(count_of(a[0], &page) && page >= 1 && page <= INT32_MAX && count_of(a[5], &tokens) && tt.size[1] <= INT32_MAX);
-    UNLESS(PyTuple_Check(a[6]) && PyTuple_GET_SIZE(a[6]) == 6);
+    UNLESS(count_of(a[0], &page) && page >= 1 && page <= INT32_MAX && count_of(a[5], &tokens) && tokens >= 0 && tt.size[1] <= INT32_MAX && PyTuple_Check(a[6]));
     const int64_t size[6] = {tf.size[0] + 1, tf.size[0], tokens, tokens, tokens, 1};
-    for (int i = 0; i < 6; ++i) UNLESS(of_type(PyTuple_GET_ITEM(a[6], i), 1, i == 2 ? t_int64 : t_int32, &out[i]) && out[i].size[0] == size[i]);
+    if (PyTuple_GET_SIZE(a[6]) == 2) {
+        UNLESS(of_type(PyTuple_GET_ITEM(a[6], 0), 1, t_int32, &out[0]) && of_type(PyTuple_GET_ITEM(a[6], 1), 1, t_int64, &out[2]));
+        UNLESS(tokens <= INT32_MAX && out[0].size[0] == 2 * tf.size[0] + 2 + 2 * tokens && out[2].size[0] == tokens);
+        out[1].data = (int32_t *)out[0].data + size[0];
+        out[5].data = (int32_t *)out[1].data + size[1];
+        out[3].data = (int32_t *)out[5].data + 1;
+        out[4].data = (int32_t *)out[3].data + tokens;
+    } else {
+        UNLESS(PyTuple_GET_SIZE(a[6]) == 6);
+        for (int i = 0; i < 6; ++i) UNLESS(of_type(PyTuple_GET_ITEM(a[6], i), 1, i == 2 ? t_int64 : t_int32, &out[i]) && out[i].size[0] == size[i]);
+    }
     UNLESS(stream_of(a[7], &stream));
     memset(&g, 0, sizeof(g));
     g.requests = tf.size[0];

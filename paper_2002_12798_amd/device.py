@@ -212,12 +212,19 @@ class Assigned(NamedTuple):
     taken: torch.Tensor      # [1] int32: pages needed from the list
 
 
+def _assigned_room(requests, n_tokens, device):
+    """The two buffers that an assignment's tensors are parts of."""
+    return torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=device), torch.empty(n_tokens, dtype=torch.int64, device=device)
+
+
+def _assigned_in(room, requests, n_tokens) -> Assigned:
+    begin, length, taken, position, owner = room[0].split_with_sizes((requests + 1, requests, 1, n_tokens, n_tokens))
+    return Assigned(begin, length, room[1], position, owner, taken)
+
+
 def assigned_buffers(requests, n_tokens, like=None) -> Assigned:
     """Room for a step's assignment, for a program that keeps it from step to step (as a captured graph has to)."""
-    dev = require_gpu() if like is None else like.device
-    whole = torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=dev)
-    begin, length, taken, position, owner = whole.split_with_sizes((requests + 1, requests, 1, n_tokens, n_tokens))
-    return Assigned(begin, length, torch.empty(n_tokens, dtype=torch.int64, device=dev), position, owner, taken)
+    return _assigned_in(_assigned_room(requests, n_tokens, require_gpu() if like is None else like.device), requests, n_tokens)
 
 
 def _made_on(stream):
@@ -233,12 +240,11 @@ def cache_assign(page_size, cached, fresh, table, free_pages, n_tokens, out=None
     new pages are taken from the head of free_pages into `table`, which is changed in place.  All int32."""
     what = "amap_cache_assign"
     if stream is None and type(n_tokens) is int and n_tokens >= 0 and isinstance(fresh, torch.Tensor) and fresh.dim() == 1 and fresh.is_cuda:
-        if out is None:
-            out = assigned_buffers(fresh.size(0), n_tokens, fresh)
-        st = _assign(page_size, cached, fresh, table, free_pages, n_tokens, out, None)
+        room = _assigned_room(len(fresh), n_tokens, fresh.device) if out is None else out
+        st = _assign(page_size, cached, fresh, table, free_pages, n_tokens, room, None)
         if st >= 0:
             B._check(st, what)
-            return out
+            return _assigned_in(room, len(fresh), n_tokens) if out is None else out
     n = _on_gpu(fresh, torch.int32, 1, what, "fresh").size(0)
     _on_gpu(table, torch.int32, 2, what, "table")
     _on_gpu(free_pages, torch.int32, 1, what, "free_pages")
