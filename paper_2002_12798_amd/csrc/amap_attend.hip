@@ -30,7 +30,7 @@ constexpr int kTokens = 32;        // of a wavefront's step
 constexpr int kColumns = 16;       // queries of a workgroup at a time (8 where their weights' second parts have the others)
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 constexpr uint32_t kBegin = 3;             // what beginning and ending a segment counts for in a share, in tiles
-constexpr uint32_t kMostJoining = 4096;    // workgroups of a join
+constexpr uint32_t kMostJoining = 8192;    // workgroups of a join
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
 struct AttendArgs {
@@ -550,9 +550,9 @@ struct JoinArgs {
     uint32_t parts, segments, blocks;
 };
 
-template <class T, int DP>
-__global__ __launch_bounds__(256) void amap_attend_join_kernel(const JoinArgs a) {
-    constexpr uint32_t kPart = kColumns * (DP + 2), kLanes = DP / 4, kSlots = 256 / kLanes;   // slots: of a row's lanes
+template <class T, int DP, int THREADS>
+__global__ __launch_bounds__(THREADS) void amap_attend_join_kernel(const JoinArgs a) {
+    constexpr uint32_t kPart = kColumns * (DP + 2), kLanes = DP / 4, kSlots = THREADS / kLanes;   // slots: of a row's lanes
     __shared__ float tops[kSlots], sums[kSlots];
     __shared__ f32x4 results[kSlots][kLanes];
     const uint32_t slot = threadIdx.x / kLanes, lane = threadIdx.x % kLanes, d = 4u * lane;
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(256) void amap_attend_join_kernel(const JoinArgs a)
         float high = -INFINITY, sum = 0.f;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         if (way < ways && c < rows) {
-#pragma unroll 4
+#pragma unroll 8
             for (uint32_t p = way; p < s.count; p += ways) {
                 const float *const part = first + (size_t)(p ? 2u * p : 1u) * kPart;
                 const float m = part[c], l = part[kColumns + c];
@@ -624,14 +624,18 @@ amap_status attend(AttendArgs a, const Cut &cut, hipStream_t s) {
     }
     hipError_t e = launch_kernel<amap_attend_kernel<F>>(dim3(cut.groups), dim3(64), F::LDS, s, a);
     if (e != hipSuccess || !cut.splits) return launched(e, "amap_attend_kernel");
-    // as many lanes to a row as there are pieces of a segment, if all are split alike
-    const uint32_t segments = a.requests * a.segments, rows = a.columns < a.group ? a.columns : a.group, slots = 256u / (F::DP / 4), pieces = 1u + cut.groups / segments;
-    uint32_t at_once = slots / pieces;
+    // As many lanes to a row as there are pieces of a segment, if all are split alike; a wavefront at a time where those are few (six pieces of
+    // each of 253 segments: 7.3 us by 256 threads, 5.3 by 64).
+    const uint32_t segments = a.requests * a.segments, rows = a.columns < a.group ? a.columns : a.group, pieces = 1u + cut.groups / segments;
+    const bool few = pieces <= 16;
+    uint32_t at_once = (few ? 64u : 256u) / (F::DP / 4) / pieces;
     at_once = at_once < 1 ? 1 : at_once > rows ? rows : at_once;
     const uint32_t parts = (rows + at_once - 1) / at_once, work = segments * parts;
     const JoinArgs j{a.parts, a.splits, a.out, a.lse, a.v_scale, a.out_token, a.out_head, work, at_once, a.columns, a.group, a.heads, a.dim, make_fastdiv(parts), a.by_segments, a.by_blocks,
                      parts, a.segments, a.blocks};
-    e = launch_kernel<amap_attend_join_kernel<typename F::T, F::DP>>(dim3(work < kMostJoining ? work : kMostJoining), dim3(256), 0, s, j);
+    const dim3 grid(work < kMostJoining ? work : kMostJoining);
+    e = few ? launch_kernel<amap_attend_join_kernel<typename F::T, F::DP, 64>>(grid, dim3(64), 0, s, j)
+            : launch_kernel<amap_attend_join_kernel<typename F::T, F::DP, 256>>(grid, dim3(256), 0, s, j);
     return launched(e, "amap_attend_join_kernel");
 }
 

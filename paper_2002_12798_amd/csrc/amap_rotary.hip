@@ -132,10 +132,23 @@ __device__ __forceinline__ void store_as(uint32_t type, char *at, const float (&
     }
 }
 
-// T: the rows' type; BYTES: of one access to them; HALVES: a pair's elements in two accesses; STREAM: stores past the caches
-template <class T, int BYTES, bool HALVES, bool STREAM>
+// How a pair's elements come to one lane: beside one another in one access (or nothing is turned); in two accesses, one to each half of the pairs; or in
+// two neighbouring lanes, one access each, which hand each other half of what they have.  The last covers rows without gaps where a half is no
+// whole number of 64-byte pieces (heads of 80, 40 pairs: 20.4 -> 15.2 us over 64 MB), and costs the others a little.
+enum Pairs { kBeside = 0, kHalves = 1, kLanes = 2 };
+
+// the neighbouring lane's
+__device__ __forceinline__ uint32_t of_neighbour(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false); }   // quad_perm 1, 0, 3, 2
+
+// `b` where the mask is all ones, else `a` (a choice between elements of an array, written as one, went through memory)
+__device__ __forceinline__ uint32_t choose(uint32_t mask, uint32_t a, uint32_t b) { return (a & ~mask) | (b & mask); }
+__device__ __forceinline__ float choose(uint32_t mask, float a, float b) { return __uint_as_float(choose(mask, __float_as_uint(a), __float_as_uint(b))); }
+
+// T: the rows' type; BYTES: of one access to them; STREAM: stores past the caches
+template <class T, int BYTES, Pairs PAIRS, bool STREAM>
 __global__ __launch_bounds__(kMostThreads) void amap_turn_kernel(const TurnArgs a) {
     constexpr int V = BYTES / T::bytes, U = kAtOnce;
+    constexpr bool HALVES = PAIRS == kHalves;
     typedef typename Piece<BYTES>::type piece;
     extern __shared__ char lds[];
     int64_t *const place = reinterpret_cast<int64_t *>(lds);                          // [group]: of a token's row in the cache, -1: none
@@ -152,9 +165,10 @@ __global__ __launch_bounds__(kMostThreads) void amap_turn_kernel(const TurnArgs 
         const TurnJob &job = a.job[j];
         const uint32_t head = fdiv(u, job.by_head);
         u -= head * job.per_head;
-        const uint32_t halves = HALVES && job.turns ? a.pairs / V : 0u;
+        const uint32_t halves = HALVES && job.turns ? a.pairs / V : 0u, second = u & 1u;   // second: (neighbouring lanes) of the pairs' second elements
         const bool turned = HALVES ? u < halves : job.turns && u * V < 2u * a.pairs;
-        const uint32_t at = u < halves ? u * V : (u + halves) * V;   // its first element: of the first halves, or of what lies behind both
+        // its first element: of the first halves, or of what lies behind both
+        const uint32_t at = PAIRS == kLanes && turned ? (u >> 1) * V + second * a.pairs : u < halves ? u * V : (u + halves) * V;
         const char *const src = job.src + ((int64_t)(t0 + beside) * job.src_token + (int64_t)head * job.src_head + at) * T::bytes;
         const int64_t step = (int64_t)a.beside * job.src_token * T::bytes;
         piece x[U], y[U];
@@ -212,6 +226,31 @@ __global__ __launch_bounds__(kMostThreads) void amap_turn_kernel(const TurnArgs 
                     }
                     store_as<V, STREAM>(type, dst + a.pairs * es, w);
                 }
+            } else if constexpr (PAIRS == kLanes) {
+                // first elements 0 .. V - 1 here and the second ones next door: this lane takes pairs 0 .. V / 2 - 1, the other one the rest
+                if (turned) {
+                    constexpr int W = BYTES / 8;   // words of half a piece
+                    const uint32_t mask = 0u - second;
+                    uint32_t got[W];
+#pragma unroll
+                    for (int e = 0; e < W; ++e) got[e] = of_neighbour(choose(mask, x[k][W + e], x[k][e]));
+                    float f[V / 2], b[V / 2];
+                    const uint32_t pair = (u >> 1) * V + second * (V / 2);
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e) {
+                        const float own = choose(mask, v[e], v[V / 2 + e]), its = widen<T>(reinterpret_cast<const char *>(got) + e * T::bytes);
+                        const float first = choose(mask, own, its), other = choose(mask, its, own);
+                        const float2 c = cs[pair + e];
+                        f[e] = first * c.x - other * c.y;
+                        b[e] = other * c.x + first * c.y;
+                    }
+#pragma unroll
+                    for (int e = 0; e < V / 2; ++e) {
+                        const float its = __uint_as_float(of_neighbour(__float_as_uint(choose(mask, b[e], f[e]))));
+                        v[e] = choose(mask, f[e], its);
+                        v[V / 2 + e] = choose(mask, its, b[e]);
+                    }
+                }
             } else if constexpr (V > 1) {
                 if (turned) {
 #pragma unroll
@@ -256,17 +295,22 @@ struct Way {
     const float *scale;
 };
 
+template <class T, int BYTES, Pairs PAIRS, bool STREAM>
+hipError_t turn(const TurnArgs &g, uint32_t grid, uint32_t threads, uint32_t lds, hipStream_t s) {
+    return launch_kernel<amap_turn_kernel<T, BYTES, PAIRS, STREAM>>(dim3(grid), dim3(threads), lds, s, g);
+}
 template <class T, int BYTES, bool STREAM>
-hipError_t turn(bool halves, const TurnArgs &g, uint32_t grid, uint32_t threads, uint32_t lds, hipStream_t s) {
-    return halves ? launch_kernel<amap_turn_kernel<T, BYTES, true, STREAM>>(dim3(grid), dim3(threads), lds, s, g)
-                  : launch_kernel<amap_turn_kernel<T, BYTES, false, STREAM>>(dim3(grid), dim3(threads), lds, s, g);
+hipError_t turn_by(Pairs pairs, const TurnArgs &g, uint32_t grid, uint32_t threads, uint32_t lds, hipStream_t s) {
+    if constexpr (BYTES == 16)
+        if (pairs == kLanes) return turn<T, BYTES, kLanes, STREAM>(g, grid, threads, lds, s);
+    return pairs == kHalves ? turn<T, BYTES, kHalves, STREAM>(g, grid, threads, lds, s) : turn<T, BYTES, kBeside, STREAM>(g, grid, threads, lds, s);
 }
 template <class T>
-hipError_t turn_by(int bytes, bool halves, bool stream, const TurnArgs &g, uint32_t grid, uint32_t threads, uint32_t lds, hipStream_t s) {
-    if (bytes == 16) return stream ? turn<T, 16, true>(halves, g, grid, threads, lds, s) : turn<T, 16, false>(halves, g, grid, threads, lds, s);
-    if (bytes == 8) return turn<T, 8, false>(halves, g, grid, threads, lds, s);
-    if (T::bytes == 2 && bytes == 2) return turn<T, T::bytes, false>(halves, g, grid, threads, lds, s);
-    return turn<T, 4, false>(halves, g, grid, threads, lds, s);
+hipError_t turn_of(int bytes, Pairs pairs, bool stream, const TurnArgs &g, uint32_t grid, uint32_t threads, uint32_t lds, hipStream_t s) {
+    if (bytes == 16) return stream ? turn_by<T, 16, true>(pairs, g, grid, threads, lds, s) : turn_by<T, 16, false>(pairs, g, grid, threads, lds, s);
+    if (bytes == 8) return turn_by<T, 8, false>(pairs, g, grid, threads, lds, s);
+    if (T::bytes == 2 && bytes == 2) return turn_by<T, T::bytes, false>(pairs, g, grid, threads, lds, s);
+    return turn_by<T, 4, false>(pairs, g, grid, threads, lds, s);
 }
 
 // Threads of a workgroup for rows of so many units: as few lanes as possible without one (64 .. 512 in steps of 64; 256 where others are no better).
@@ -324,7 +368,11 @@ amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope 
         g.n_slots = cache->n_pages * cache->page_size;
         g.page = (uint32_t)cache->page_size;
     }
-    const uint32_t per_head = (uint32_t)(dim / (int)width), halves = rope && !rope->interleaved ? (uint32_t)rope->pairs / (uint32_t)width : 0u;
+    const uint32_t per_head = (uint32_t)(dim / (int)width), all_halves = rope && !rope->interleaved ? (uint32_t)rope->pairs / (uint32_t)width : 0u;
+    // pairs in neighbouring lanes: the units of one head, and of all in front of it, have to be even in number
+    Pairs pairs = all_halves ? kHalves : kBeside;
+    if (all_halves && (int)width * es == 16 && (uint64_t)rope->pairs * es % 64 && per_head % 2 == 0) pairs = kLanes;
+    const uint32_t halves = pairs == kHalves ? all_halves : 0u;
     uint64_t units = 0;
     for (int i = 0; i < n; ++i) {
         const Way &w = way[i];
@@ -371,20 +419,19 @@ amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope 
     const int bytes = (int)width * es;
     // Past the caches where every run of a store is whole 64-byte pieces at both ends: [65536,16,128] bf16 106 -> 98 us, [16391,8,128] k and v stored
     // 34 -> 25, but rows of 160 bytes in two halves of 80 20.4 -> 24.
-    const bool paired = rope && !rope->interleaved;
     uint64_t runs = 0;
     for (int i = 0; i < n; ++i) {
         const Way &w = way[i];
         const uint64_t out = (uint64_t)bytes_of(w.out);
         // (heads that follow one another are one run, unless their halves are stored apart)
-        const bool apart = paired && w.turns, joined = !apart && w.head == dim;
+        const bool apart = pairs == kHalves && w.turns, joined = !apart && w.head == dim;
         runs |= reinterpret_cast<uintptr_t>(w.dst) | out * ((uint64_t)w.token | (uint64_t)w.page);
         runs |= out * (joined ? (uint64_t)dim * (uint64_t)w.in->heads : (uint64_t)w.head | (uint64_t)dim | (apart ? (uint64_t)rope->pairs : 0u));
     }
     const bool past = runs % 64 == 0;
-    const hipError_t e = type == AMAP_F32    ? turn_by<F32>(bytes, paired, past, g, grid, threads, lds, s)
-                         : type == AMAP_BF16 ? turn_by<Bf16>(bytes, paired, past, g, grid, threads, lds, s)
-                                             : turn_by<F16>(bytes, paired, past, g, grid, threads, lds, s);
+    const hipError_t e = type == AMAP_F32    ? turn_of<F32>(bytes, pairs, past, g, grid, threads, lds, s)
+                         : type == AMAP_BF16 ? turn_of<Bf16>(bytes, pairs, past, g, grid, threads, lds, s)
+                                             : turn_of<F16>(bytes, pairs, past, g, grid, threads, lds, s);
     return launched(e, "amap_turn_kernel");
 }
 
