@@ -156,13 +156,41 @@ __global__ __launch_bounds__(kMostThreads) void amap_turn_kernel(const TurnArgs 
     const uint32_t tid = threadIdx.x, block = fdiv(blockIdx.x, a.by_split), split = blockIdx.x - block * a.splits;
     const uint32_t t0 = block * a.group, count = min(a.group, a.tokens - t0);
     const uint32_t beside = fdiv(tid, a.by_width), in = tid - beside * a.width;
+    // the first of this lane's angles: asked for in front of the rows, so that it can be made while they are on their way
+    auto axis_of = [&](uint32_t p) __attribute__((always_inline)) {
+        uint32_t axis = 0;
+#pragma unroll
+        for (int k = 0; k + 1 < AMAP_MAX_AXES; ++k) axis += p >= a.axis_end[k];
+        return axis;
+    };
+    const uint32_t angles = count * a.pairs;
+    int32_t position = 0;
+    float freq = 0.f;
+    if (tid < angles) {
+        const uint32_t t = fdiv(tid, a.by_pairs), p = tid - t * a.pairs;
+        position = a.position[axis_of(p) * a.axis_stride + t0 + t];
+        freq = a.freq[p];
+    }
     for (uint32_t round = split; round < a.rounds; round += a.splits) {
         // ---- this lane's unit
         uint32_t u = round * a.width + in, j = 0;
         const bool mine = u < a.units && beside < a.beside;
         if (!mine) u = 0;
-        while (j + 1 < a.n_jobs && u >= a.job[j].units) u -= a.job[j++].units;
-        const TurnJob &job = a.job[j];
+        // Its tensor, put together from scalars: read by an index that differs from lane to lane, each field would be a load of its own, and those in the
+        // last loop would wait for the stores in front of them.
+        TurnJob job = a.job[0];
+        if (a.n_jobs > 1) {
+#pragma unroll
+            for (int k = 0; k + 1 < kMaxJobs; ++k) {
+                const bool on = (uint32_t)k + 1 < a.n_jobs && j == (uint32_t)k && u >= a.job[k].units;
+                const TurnJob &to = a.job[k + 1];
+                if (on) {
+                    u -= a.job[k].units;
+                    j = k + 1;
+                    job = to;
+                }
+            }
+        }
         const uint32_t head = fdiv(u, job.by_head);
         u -= head * job.per_head;
         const uint32_t halves = HALVES && job.turns ? a.pairs / V : 0u, second = u & 1u;   // second: (neighbouring lanes) of the pairs' second elements
@@ -184,12 +212,13 @@ __global__ __launch_bounds__(kMostThreads) void amap_turn_kernel(const TurnArgs 
                     const int64_t slot = a.slot[t0 + i], page = slot / a.page;   // (the caches' strides are the first job's)
                     place[i] = slot >= 0 && slot < a.n_slots ? page * a.job[0].dst_page + (slot - page * a.page) * a.job[0].dst_token : -1;
                 }
-            for (uint32_t i = tid; i < count * a.pairs; i += blockDim.x) {
-                const uint32_t t = fdiv(i, a.by_pairs), p = i - t * a.pairs;
-                uint32_t axis = 0;
-#pragma unroll
-                for (int k = 0; k + 1 < AMAP_MAX_AXES; ++k) axis += p >= a.axis_end[k];
-                const double turns = (double)a.position[axis * a.axis_stride + t0 + t] * (double)a.freq[p] * 0.15915494309189533577;   // 1 / (2 pi)
+            for (uint32_t i = tid; i < angles; i += blockDim.x) {
+                if (i != tid) {
+                    const uint32_t t = fdiv(i, a.by_pairs), p = i - t * a.pairs;
+                    position = a.position[axis_of(p) * a.axis_stride + t0 + t];
+                    freq = a.freq[p];
+                }
+                const double turns = (double)position * (double)freq * 0.15915494309189533577;   // 1 / (2 pi)
                 float s, c;
                 sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
                 angle[i] = make_float2(c, a.inverse ? -s : s);
