@@ -346,6 +346,7 @@ hipError_t turn_of(int bytes, Pairs pairs, bool stream, const TurnArgs &g, uint3
 uint32_t threads_for(uint64_t units) {
     uint32_t best = 256;
     double most = 0.0;
+    if (units > 256 && units <= kMostThreads) return (uint32_t)(units + 63) / 64 * 64;   // all of a token's at once
     for (uint32_t n : {256u, 320u, 384u, 448u, 512u, 192u, 128u}) {
         const double held = units <= n ? (double)(n / units * units) / n : (double)units / (double)((units + n - 1) / n * n);
         if (held > most + 0.03) most = held, best = n;
@@ -400,7 +401,10 @@ amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope 
     const uint32_t per_head = (uint32_t)(dim / (int)width), all_halves = rope && !rope->interleaved ? (uint32_t)rope->pairs / (uint32_t)width : 0u;
     // pairs in neighbouring lanes: the units of one head, and of all in front of it, have to be even in number
     Pairs pairs = all_halves ? kHalves : kBeside;
-    if (all_halves && (int)width * es == 16 && (uint64_t)rope->pairs * es % 64 && per_head % 2 == 0) pairs = kLanes;
+    // (Whole pieces as well where they are read and written far beyond the caches: 134 MB in and out 51.6 -> 51.2 us, 268 MB 98.6 -> 94.7, heads of 64 52 -> 47;
+    // 67 MB 23.4 against 26.4, 8 MB 8.3 against 10.)
+    const bool far_beyond = n == 1 && tokens * way[0].in->heads * dim * es >= ((int64_t)128 << 20);
+    if (all_halves && (int)width * es == 16 && per_head % 2 == 0 && ((uint64_t)rope->pairs * es % 64 || far_beyond)) pairs = kLanes;
     const uint32_t halves = pairs == kHalves ? all_halves : 0u;
     uint64_t units = 0;
     for (int i = 0; i < n; ++i) {
@@ -439,7 +443,7 @@ amap_status run(const Way *way, int n, int64_t tokens, int dim, const amap_rope 
     threads = (g.width * g.beside + 63u) / 64u * 64u;
     g.rounds = (g.units + g.width - 1) / g.width;
     const uint64_t blocks = ((uint64_t)tokens + g.group - 1) / g.group;
-    g.splits = blocks >= 512 ? 1 : g.rounds;
+    g.splits = blocks >= 2048 ? 1 : g.rounds;
     if (blocks * g.splits >= (1u << 31)) return refuse("too many tokens for one launch");
     g.by_split = make_fastdiv(g.splits);
     const uint32_t lds = g.group * g.pairs * 8u + (slot ? 8u * g.group : 0u), grid = (uint32_t)(blocks * g.splits);
