@@ -156,9 +156,9 @@ except ImportError as e:
 
     class _call:
         """The extension's functions, none of which takes a call."""
-        library = torch = paged = staticmethod(lambda *functions: None)
+        library = torch = staticmethod(lambda *functions: None)
         current_stream = staticmethod(lambda: None)
-        execute = execute_multi = gemm = gather = rotary = append = attend = assign = staticmethod(lambda *args: -1)
+        execute = execute_multi = gemm = gather = staticmethod(lambda *args: -1)
 
 _call.library(*(C.cast(f, _vp).value for f in (_L.amap_execute, _L.amap_execute_multi, _L.amap_gemm_fused, _L.amap_gemm_fused_store,
                                                _L.amap_gemm_mapped, _L.amap_gemm_gather)))

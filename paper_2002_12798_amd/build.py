@@ -13,6 +13,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libamap.so")
 # CPython extension, from a Python call to the library: its name holds the interpreter's ABI, and another one looks for another name
 CALL = os.path.join(_HERE, "_amap_call" + sysconfig.get_config_var("EXT_SUFFIX"))
+# the same for calls on torch's tensors as they are: for one torch as well, which the module names
+PAGED_CALL = os.path.join(_HERE, "_amap_paged_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 SOURCES = ["amap_compose.cpp", "amap_graph.cpp", "amap_layout.cpp", "amap_host.cpp", "amap_plan.cpp", "amap_plan_check.cpp", "amap_kernels.hip",
            "amap_gemm.hip", "amap_gemm_ring.hip", "amap_cache.hip", "amap_rotary.hip", "amap_attend.hip"]
@@ -63,6 +65,7 @@ def build_lib(verbose: bool = False, extra=()) -> str:
         os.remove(LIB)
         raise RuntimeError("; ".join(wrong))
     build_call()
+    build_paged_call()
     return LIB
 
 
@@ -75,12 +78,32 @@ def build_call():
             os.remove(CALL)   # of another state of the source
         print(f"{CALL} not built (no {lacks}): Python calls go through ctypes", file=sys.stderr)
         return None
-    subprocess.run(["gcc", "-O2", "-std=c99", "-fPIC", "-shared", "-Wall", "-Wextra", "-I", include, "-I", os.path.join(ROOT, "include"),
-                    os.path.join(CSRC, "amap_call.c"), "-o", CALL, "-lm"], check=True)
+    subprocess.run(["gcc", "-O2", "-std=c99", "-fPIC", "-shared", "-Wall", "-Wextra", "-I", include,
+                    os.path.join(CSRC, "amap_call.c"), "-o", CALL], check=True)
     untagged = os.path.join(_HERE, "_amap_call.so")   # built so before: any interpreter would load it
     if os.path.exists(untagged):
         os.remove(untagged)
     return CALL
+
+
+def build_paged_call():
+    """The extension's path, or None where it cannot be built: the calls around the paged cache then go through ctypes."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    include = [os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"), sysconfig.get_path("include")]
+    lacks = "g++" if not shutil.which("g++") else next((d for d in include if not os.path.isdir(d)), None)
+    if os.path.exists(PAGED_CALL):
+        os.remove(PAGED_CALL)   # of another state of the source, or another torch
+    if not lacks:
+        r = subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                            f'-DAMAP_TORCH_VERSION="{torch.__version__}"', *[x for d in include for x in ("-isystem", d)], "-I", os.path.join(ROOT, "include"),
+                            os.path.join(CSRC, "amap_paged_call.cpp"), "-o", PAGED_CALL, "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"],
+                           stderr=subprocess.PIPE, text=True)
+        if r.returncode == 0:
+            return PAGED_CALL
+        lacks = r.stderr.strip().splitlines()[-1] if r.stderr.strip() else "a compiler that takes it"
+    print(f"{PAGED_CALL} not built ({lacks}): calls around the paged cache go through ctypes", file=sys.stderr)
+    return None
 
 
 # Wavefronts per SIMD of the map kernels.  They are bound by memory and every form inlined into amap_pieces_kernel shares its

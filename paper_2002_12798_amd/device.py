@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import contextlib
 import operator
+import warnings
 from typing import NamedTuple
 
 import numpy as np
@@ -112,12 +113,6 @@ def gemm_fused(a_src: torch.Tensor, a_map, w: torch.Tensor, out=None, stream=Non
 # (a tensor of 16-bit words holds bf16 bits, as everywhere in this package)
 _ELEMENT = {torch.float32: B.AMAP_F32, torch.bfloat16: B.AMAP_BF16, torch.int16: B.AMAP_BF16, torch.float16: B.AMAP_F16, torch.float8_e4m3fn: B.AMAP_E4M3}
 
-# The ordinary call goes through the extension (its answer is the library's status); what it does not take (-1) goes the long way below, which says why.
-if hasattr(B._L, "amap_rotary"):
-    B._call.paged(*(B.C.cast(getattr(B._L, name), B.C.c_void_p).value for name in ("amap_cache_assign", "amap_rotary", "amap_cache_append", "amap_cache_attend",
-                                                                                   "amap_cache_attend_workspace")),
-                  torch.int32, torch.int64, torch.float32, torch.uint8, tuple(_ELEMENT.items()))
-_rotary, _append, _attend, _assign = B._call.rotary, B._call.append, B._call.attend, B._call.assign
 _capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_current_stream_capturing)
 
 
@@ -212,19 +207,40 @@ class Assigned(NamedTuple):
     taken: torch.Tensor      # [1] int32: pages needed from the list
 
 
-def _assigned_room(requests, n_tokens, device):
-    """The two buffers that an assignment's tensors are parts of."""
-    return torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=device), torch.empty(n_tokens, dtype=torch.int64, device=device)
-
-
-def _assigned_in(room, requests, n_tokens) -> Assigned:
-    begin, length, taken, position, owner = room[0].split_with_sizes((requests + 1, requests, 1, n_tokens, n_tokens))
-    return Assigned(begin, length, room[1], position, owner, taken)
-
-
 def assigned_buffers(requests, n_tokens, like=None) -> Assigned:
     """Room for a step's assignment, for a program that keeps it from step to step (as a captured graph has to)."""
-    return _assigned_in(_assigned_room(requests, n_tokens, require_gpu() if like is None else like.device), requests, n_tokens)
+    dev = require_gpu() if like is None else like.device
+    words = torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=dev)
+    begin, length, position, owner, taken = words.split_with_sizes((requests + 1, requests, n_tokens, n_tokens, 1))
+    return Assigned(begin, length, torch.empty(n_tokens, dtype=torch.int64, device=dev), position, owner, taken)
+
+
+class _NoCalls:
+    """The extension's functions, none of which takes a call."""
+    assign = rotary = append = attend = staticmethod(lambda *args: None)
+
+
+def _native_calls():
+    """The calls on tensors as they are (amap_paged_call.cpp), if they are built for this torch and the library has what they call: their answer is the
+    outputs or the library's status, or None for a call that they do not take, which goes the long way below; that says why."""
+    if not hasattr(B._L, "amap_rotary") or _raw_stream is None:
+        return _NoCalls
+    try:
+        from . import _amap_paged_call as calls
+    except ImportError as e:
+        warnings.warn(f"{e}: calls around the paged cache go through ctypes; run `python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning)
+        return _NoCalls
+    if calls.torch_version != torch.__version__:
+        warnings.warn(f"_amap_paged_call is built for torch {calls.torch_version}: calls around the paged cache go through ctypes", RuntimeWarning)
+        return _NoCalls
+    calls.library(*(B.C.cast(getattr(B._L, name), B.C.c_void_p).value for name in ("amap_cache_assign", "amap_rotary", "amap_cache_append", "amap_cache_attend",
+                                                                                   "amap_cache_attend_workspace")),
+                  Assigned, _raw_stream, _get_device, torch.cuda.is_initialized, _capturing)
+    return calls
+
+
+_native = _native_calls()
+_native_assign, _native_rotary, _native_append, _native_attend = _native.assign, _native.rotary, _native.append, _native.attend
 
 
 def _made_on(stream):
@@ -239,12 +255,9 @@ def cache_assign(page_size, cached, fresh, table, free_pages, n_tokens, out=None
     """Pages, slots and positions for a step in which request r adds fresh[r] tokens to its cached[r] (None: none yet):
     new pages are taken from the head of free_pages into `table`, which is changed in place.  All int32."""
     what = "amap_cache_assign"
-    if stream is None and type(n_tokens) is int and n_tokens >= 0 and isinstance(fresh, torch.Tensor) and fresh.dim() == 1 and fresh.is_cuda:
-        room = _assigned_room(len(fresh), n_tokens, fresh.device) if out is None else out
-        st = _assign(page_size, cached, fresh, table, free_pages, n_tokens, room, None)
-        if st >= 0:
-            B._check(st, what)
-            return _assigned_in(room, len(fresh), n_tokens) if out is None else out
+    done = _native_assign(page_size, cached, fresh, table, free_pages, n_tokens, out, stream)
+    if done is not None:
+        return done if type(done) is not int else B._check(done, what)
     n = _on_gpu(fresh, torch.int32, 1, what, "fresh").size(0)
     _on_gpu(table, torch.int32, 2, what, "table")
     _on_gpu(free_pages, torch.int32, 1, what, "free_pages")
@@ -269,12 +282,9 @@ def rotary(x, rope, position, out=None, inverse=False, stream=None) -> torch.Ten
     """out = x [tokens, heads, head_dim] turned to its positions ([tokens] or [axes, tokens], int32); inverse: turned back, the
     gradient.  out may be x itself."""
     what = "amap_rotary"
-    if out is None and stream is None and isinstance(x, torch.Tensor) and x.is_cuda:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    st = _rotary(x, rope, position, out, inverse, stream)
-    if st >= 0:
-        B._check(st, what)
-        return out
+    done = _native_rotary(x, rope, position, out, inverse, stream)
+    if done is not None:
+        return done if type(done) is not int else B._check(done, what)
     a = _rows(x, what, "x")
     if out is None:
         with _made_on(stream):
@@ -290,12 +300,9 @@ def cache_append(cache, k, v, slot, rope=None, position=None, q=None, q_out=None
     """k and v [tokens, kv_heads, head_dim] into the cache at slot [tokens] (int64; outside the cache: left out), k turned by the
     rope on the way, if there is one, and q into q_out (allocated if None; returned)."""
     what = "amap_cache_append"
-    if q is not None and q_out is None and stream is None and isinstance(q, torch.Tensor) and q.is_cuda:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    st = _append(cache, k, v, slot, rope, position, q, q_out, stream)
-    if st >= 0:
-        B._check(st, what)
-        return q_out
+    done = _native_append(cache, k, v, slot, rope, position, q, q_out, stream)
+    if done is not None:
+        return (None if done is True else done) if type(done) is not int else B._check(done, what)
     a, b = _rows(k, what, "k"), _rows(v, what, "v")
     tokens, dim = k.size(0), cache.k.size(3)
     if v.size(0) != tokens or k.size(2) != dim or v.size(2) != dim or (q is not None and isinstance(q, torch.Tensor) and (q.size(0) != tokens or q.size(-1) != dim)):
@@ -321,18 +328,9 @@ def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=No
     `window` of them) that table [requests, width] (int32) leads to.  scale: 1 / sqrt(head_dim) if None.  A request that sees nothing has
     rows of 0 and lse -inf.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it."""
     what = "amap_cache_attend"
-    if stream is None and isinstance(q, torch.Tensor) and q.is_cuda and q.dim() == 3:
-        if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        if lse is None:
-            lse = q.new_empty((q.size(0), q.size(1)), dtype=torch.float32)
-        work = workspace
-        if work is None and not _capturing():
-            work = cache._work.get(current_stream())
-        st = _attend(cache, q, table, length, scale, window, out, lse, work, None)
-        if st >= 0:
-            B._check(st, what)
-            return out, lse
+    done = _native_attend(cache, q, table, length, scale, window, out, lse, workspace, stream)
+    if done is not None:
+        return done if type(done) is not int else B._check(done, what)
     a = _rows(q, what, "q")
     n, heads, dim = q.shape
     _on_gpu(table, torch.int32, 2, what, "table")
