@@ -686,7 +686,7 @@ amap_status cut_of(const amap_cache &c, int heads, int64_t requests, int table_w
     const int64_t tiles = ((int64_t)table_width * c.page_size + kTokens - 1) / kTokens;
     int64_t most;
     if (__builtin_mul_overflow(requests * cut.segments, tiles + kBegin, &most) || most >= ((int64_t)1 << 31)) return refuse("2^31 tiles of tokens or more over all requests and key heads");
-    cut.splits = tiles > 1;
+    cut.splits = tiles > 1 && requests > 0;
     cut.groups = (uint32_t)(most < 1 ? 1 : most < kUnits * per_unit ? most : kUnits * per_unit);
     cut.parts = (requests * cut.segments * (int64_t)sizeof(Split) + 15) / 16 * 16;
     cut.bytes = cut.splits ? cut.parts + (int64_t)cut.groups * (2 * 4 * kColumns * (cut.dp + 2)) : 0;
@@ -715,7 +715,7 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     if (requests == 0) return AMAP_OK;
     if (!length || (table_width && !table) || !q->data || !out->data) return AMAP_E_INVALID;
     if ((q->type != AMAP_BF16 && q->type != AMAP_F16) || out->type != q->type || (cache->type != q->type && cache->type != AMAP_E4M3)) return AMAP_E_INVALID;
-    if (out->heads != q->heads || (requests > 1 && table_stride < table_width) || table_stride > ((int64_t)1 << 40)) return AMAP_E_SHAPE;
+    if (out->heads != q->heads || table_stride < 0 || table_stride > ((int64_t)1 << 40)) return AMAP_E_SHAPE;   // (0: requests of one table row)
     const int dim = cache->head_dim, es = bytes_of(cache->type);
     const Box from = box_of(*q, requests, dim), to = box_of(*out, requests, dim), k = box_of(*cache, cache->k), v = box_of(*cache, cache->v);
     if (!from.fits || !to.fits || !to.apart) return AMAP_E_SHAPE;

@@ -112,7 +112,7 @@ def test_append(k, v, slot, rope, q, q_out, status):
 @pytest.mark.parametrize("over, args, status", [
     ({}, dict(heads=3), B.AMAP_E_SHAPE), ({}, dict(type=B.AMAP_F16), B.AMAP_E_INVALID), ({}, dict(type=B.AMAP_F32), B.AMAP_E_INVALID),
     ({}, dict(length=None), B.AMAP_E_INVALID), ({}, dict(table=None), B.AMAP_E_INVALID), ({}, dict(scale=float("nan")), B.AMAP_E_INVALID),
-    ({}, dict(window=-1), B.AMAP_E_INVALID), ({}, dict(table_stride=7), B.AMAP_E_SHAPE), ({}, dict(out=3 * AT), B.AMAP_E_ALIAS), ({}, dict(out=AT), B.AMAP_E_ALIAS),
+    ({}, dict(window=-1), B.AMAP_E_INVALID), ({}, dict(table_stride=-8), B.AMAP_E_SHAPE), ({}, {}, B.AMAP_E_INVALID), ({}, dict(out=3 * AT), B.AMAP_E_ALIAS), ({}, dict(out=AT), B.AMAP_E_ALIAS),
     ({}, dict(width=1 << 28, table_stride=1 << 28), B.AMAP_E_SHAPE), ({}, dict(requests=1 << 31), B.AMAP_E_SHAPE),
     (dict(head_dim=60), {}, B.AMAP_E_UNSUPPORTED), (dict(head_dim=264, head_stride=264, token_stride=528, page_stride=8448), {}, B.AMAP_E_UNSUPPORTED),
     (dict(token_stride=132), {}, B.AMAP_E_SHAPE), (dict(token_stride=132, page_stride=4096), {}, B.AMAP_E_UNSUPPORTED), (dict(k=AT + 8), {}, B.AMAP_E_UNSUPPORTED), (dict(type=B.AMAP_E4M3, head_dim=56), {}, B.AMAP_E_UNSUPPORTED),
@@ -122,6 +122,17 @@ def test_attend(over, args, status):
     a.update(args)
     _refuses(status, B.amap_cache_attend, _cache(**over), _rows(heads=a["heads"], type=a["type"]), a["requests"], a["table"], a["table_stride"], a["width"],
              a["length"], a["scale"], a["window"], _rows(a["out"], a["type"], a["heads"]), None, None, 0)
+
+
+def test_what_workspace_a_call_takes():
+    """None where no request can be longer than one tile; more for more workgroups, up to the chip's; 16-byte aligned."""
+    room = lambda requests, width, **over: B.amap_cache_attend_workspace(_cache(**over), 2, requests, width)  # noqa: E731
+    assert room(4, 2) == 0 and room(0, 100) == 0 and room(4, 0) == 0
+    assert 0 < room(4, 8) < room(64, 8) <= room(64, 1 << 20) == room(1024, 1 << 20) - 8 * 2 * 960
+    _refuses(B.AMAP_E_UNSUPPORTED, room, 1 << 20, 1 << 22)
+    c, need = _cache(), room(4, 8)
+    for at, size, status in ((None, 0, B.AMAP_E_INVALID), (6 * AT, need - 1, B.AMAP_E_INVALID), (6 * AT + 8, need, B.AMAP_E_UNSUPPORTED)):
+        _refuses(status, B.amap_cache_attend, c, _rows(), 4, AT, 8, 8, AT, 0.1, 0, _rows(5 * AT), None, at, size)
 
 
 def test_tensors_that_are_not_on_the_gpu():
