@@ -45,8 +45,8 @@ struct AttendArgs {
     uint32_t n_pages, page, most;                // most: tokens that a row of the table can name
     uint32_t requests, kv_heads, group, dim, pieces;   // pieces: 16-byte ones of a row
     uint32_t heads, columns, segments;           // segments of a request: kv_heads times the column blocks of one
-    FastDiv by_page, by_segments, by_blocks;
-    uint32_t blocks, least;                      // column blocks of a key head; tiles of a share, at least
+    FastDiv by_page, by_segments, by_blocks, by_groups;
+    uint32_t blocks, groups;                     // column blocks of a key head; workgroups
     uint32_t window, aligned, halves;            // aligned: q in whole 16-byte pieces; halves: 16 tokens from a multiple of 16 on lie in one page
     float scale;
 };
@@ -210,22 +210,22 @@ __device__ __forceinline__ void lds_put(uint32_t at, X x) {
 struct Seen {
     uint32_t first, past, tile, tiles, units;   // units: its tiles and what a segment of them costs besides
 };
-__device__ __forceinline__ Seen seen_of(const AttendArgs &a, uint32_t r) {
+__device__ __forceinline__ Seen seen_of(const AttendArgs &a, int32_t length) {
     Seen s;
-    s.past = min((uint32_t)max(a.length[r], 0), a.most);
+    s.past = min((uint32_t)max(length, 0), a.most);
     s.first = a.window && s.past > a.window ? s.past - a.window : 0u;
     s.tile = s.first / kTokens;
     s.tiles = (s.past + kTokens - 1) / kTokens - s.tile;
     s.units = s.tiles ? s.tiles + kBegin : 0u;
     return s;
 }
-__device__ __forceinline__ uint32_t sum_up_to(uint32_t x, uint32_t lane) {   // over the lanes, this one's included
-#pragma unroll
-    for (uint32_t d = 1; d < 64; d <<= 1) {
-        const uint32_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    return x;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t plus_shifted(uint32_t x) {
+    return x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t x) {   // over the lanes, this one's included: within rows of 16 lanes, then their last ones' sums
+    x = plus_shifted<0x118, 0xF>(plus_shifted<0x114, 0xF>(plus_shifted<0x112, 0xF>(plus_shifted<0x111, 0xF>(x))));
+    return plus_shifted<0x143, 0xC>(plus_shifted<0x142, 0xA>(x));
 }
 
 template <class F>
@@ -235,17 +235,31 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
     const uint32_t lane = threadIdx.x, g = lane >> 4, col = lane & 15u;
     const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)smem, ids = base + F::STAGES * F::STAGE;
 
+    // (the arguments that come later too: another wait for them costs 0.3 us)
+    asm volatile("" ::"s"(a.k), "s"(a.v), "s"(a.q), "s"(a.out), "s"(a.lse), "s"(a.parts), "s"(a.splits), "s"(a.k_scale), "s"(a.table), "s"(a.table_stride), "s"(a.scale), "s"(a.by_page.mul),
+                 "s"(a.by_segments.mul), "s"(a.by_blocks.mul), "s"(a.by_groups.mul), "s"(a.groups), "s"(a.window));
     // ---- the share: tiles of all requests, an equal run of them to a lane
     const uint32_t run = (a.requests + 63u) >> 6, r0 = min(lane * run, a.requests), r1 = min(r0 + run, a.requests);
+    uint32_t mine = min(blockIdx.x, a.requests - 1u);
+    asm volatile("" : "+v"(mine));
+    const int32_t own = a.length[mine];   // (asked for here, looked at below: in a scalar register it would be waited for at once)
     uint32_t units = 0;
-    for (uint32_t r = r0; r < r1; ++r) units += seen_of(a, r).units;
-    const uint32_t upto = sum_up_to(units, lane), all = __builtin_amdgcn_readlane(upto, 63) * a.segments;
-    const uint32_t share = max(a.least, (all + gridDim.x - 1) / gridDim.x);
+    int32_t length = 0;
+    for (uint32_t r = r0; r < r1; r += 4u) {
+        int32_t n[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) n[i] = a.length[min(r + i, r1 - 1u)];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) units += seen_of(a, r + i < r1 ? n[i] : 0).units;
+        length = n[0];
+    }
+    const uint32_t upto = sum_up_to(units), all = __builtin_amdgcn_readlane(upto, 63) * a.segments;
+    const uint32_t share = fdiv(max(all, 1u) - 1u, a.by_groups) + 1u;
     uint32_t u = blockIdx.x * share;
     const uint32_t end = min(u + share, all);
     // rows that see nothing, request by request over the workgroups
-    for (uint32_t r = blockIdx.x; r < a.requests; r += gridDim.x) {
-        if (seen_of(a, r).tiles) continue;
+    for (uint32_t r = blockIdx.x; r < a.requests; r += a.groups) {
+        if (__builtin_expect(seen_of(a, r == blockIdx.x ? __builtin_amdgcn_readfirstlane(own) : a.length[r]).tiles != 0u, 1)) continue;
         for (uint32_t i = lane; i < a.heads * a.dim; i += 64u) {
             const uint32_t h = i / a.dim;
             reinterpret_cast<uint16_t *>(a.out)[(int64_t)r * a.out_token + (int64_t)h * a.out_head + (i - h * a.dim)] = 0;
@@ -265,19 +279,23 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
         uint32_t before = __builtin_amdgcn_readlane(upto - units, at);
         r = at * run;
         first_of = before * a.segments;   // the request's first unit
+        length = __builtin_amdgcn_readlane(length, at);
         for (; run > 1; r += 64u) {
-            const uint32_t mine = r + lane, n = mine < a.requests ? seen_of(a, mine).units : 0u, x = before + sum_up_to(n, lane);
+            const uint32_t mine = r + lane;
+            const int32_t theirs = a.length[min(mine, a.requests - 1u)];
+            const uint32_t n = seen_of(a, mine < a.requests ? theirs : 0).units, x = before + sum_up_to(n);
             const uint64_t in = __ballot(want < x);
             if (in) {
                 const uint32_t of = (uint32_t)__builtin_ctzll(in);
                 r += of;
+                length = __builtin_amdgcn_readlane(theirs, of);
                 first_of = __builtin_amdgcn_readlane(x - n, of) * a.segments;
                 break;
             }
             before = __builtin_amdgcn_readlane(x, 63);
         }
     }
-    Seen seen = seen_of(a, r);
+    Seen seen = seen_of(a, length);
     uint32_t segment = (u - first_of) / seen.units, at = u - first_of - segment * seen.units;   // `at`: of the segment's units
 
     // ---- what does not change from segment to segment: of the 16 bytes that this lane loads, the row (as an address of ds_bpermute), the piece of
@@ -531,7 +549,7 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
         if (++segment == a.segments) {
             segment = 0;
             if (u < end) do
-                    seen = seen_of(a, ++r);
+                    seen = seen_of(a, a.length[++r]);
                 while (seen.tiles == 0);   // (there is one: units are left)
         }
     }
@@ -768,7 +786,8 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     a.by_page = make_fastdiv(a.page);
     a.by_segments = make_fastdiv(a.segments);
     a.by_blocks = make_fastdiv(a.blocks);
-    a.least = 1;
+    a.groups = cut.groups;
+    a.by_groups = make_fastdiv(a.groups);
     a.window = (uint32_t)window;
     a.aligned = q_at % 16 == 0 && (requests == 1 || q->token_stride % 8 == 0) && (q->heads == 1 || q->head_stride % 8 == 0);
     // (16 rows of a page within 32-bit byte offsets; heads of a whole form: no pieces of zeros)
