@@ -75,6 +75,7 @@ template <>
 struct Of<Bf16> {
     typedef __bf16 one;
     typedef bf16x8 eight;
+    static constexpr float UP = 0.f;   // weights are kept times 2^UP
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t x, bool high) {
         return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true))
@@ -85,6 +86,9 @@ template <>
 struct Of<F16> {
     typedef _Float16 one;
     typedef f16x8 eight;
+    // 2^15 times a weight (at most 1) is the largest that fits; without it all of a long cache's weights under 2^-25 would vanish beside one key of weight 1,
+    // 131072 of them at 2^-26 0.2 % of the sum
+    static constexpr float UP = 15.f;
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t x, bool high) {
         return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true))
@@ -420,7 +424,7 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
         f32x4 o[F::DP / 16];
 #pragma unroll
         for (int i = 0; i < F::DP / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f;   // m: the largest score less UP
         landed<0>();   // the first pages, and the queries
         load_keys(0, 0);
         load_values(0);
@@ -459,7 +463,7 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
                 for (int j = 0; j < 8; ++j) x[j] = mine >> j & 1u ? x[j] : -INFINITY;
             }
             float high = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            high = fmaxf(top_of_column(high), m);
+            high = fmaxf(top_of_column(high) - Of<typename F::T>::UP, m);
             const float from = high == -INFINITY ? 0.f : high;
             if (__any(high != m)) {
                 const float keep = __builtin_amdgcn_exp2f(m - from);

@@ -344,6 +344,22 @@ def test_attend_extreme_scores(dev):
     _check((out[3:, :1], lse[3:, :1]), tuple(x[3:, :1] for x in want), q[3:, :1], 300)
 
 
+@pytest.mark.parametrize("heads, to", [(4, F16), (16, F16), (4, E4M3)])
+def test_attend_many_small_weights_in_fp16(dev, heads, to):
+    """One key's score is 17.5 over all others, whose weights are under half of fp16's smallest step: together they are the result, as that key's value is 0."""
+    lengths, dim = [6000, 40], 64
+    cache, q, table, length = _requests(dev, 14, lengths, heads, 1, dim, 16, F16, to, "tokens")
+    q.fill_(1.0)
+    by = 1.0 if to == F16 else cache.k_scale.item()
+    for r, n in enumerate(lengths):
+        for p in range(-(-n // 16)):
+            cache.k[table[r, p], :min(16, n - 16 * p)] = 0
+        at = table[r, 1].item()
+        cache.k[at, 5] = 17.5 / 8 / by
+        cache.v[at, 5] = 0
+    _check(dev.cache_attend(cache, q, table.cuda(), length.cuda()), _expect(cache, q, table, length, dim ** -0.5), q, 6000)
+
+
 def test_attend_strided_tensors(dev):
     """q inside a packed projection at an odd place, out inside a wider tensor, a table with rows further apart, no lse kept."""
     cache, q, table, length = _requests(dev, 11, [260, 45, 130], 8, 2, 80, 16, F16, F16, "heads")
