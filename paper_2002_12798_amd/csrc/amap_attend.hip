@@ -5,7 +5,8 @@
 // kernel is built around keeping loads in flight.
 //   Work: tiles of 32 tokens, a workgroup is one wavefront.  The tiles of all requests and key heads are one line, cut into equal
 //     shares, one for each workgroup of a grid that fills the chip once: long requests are split, short ones follow one
-//     another, whatever the mix, and only where a cut falls inside a request are results joined (amap_attend_join_kernel).
+//     another, whatever the mix, and only where a cut falls inside a request are results joined (amap_attend_join_kernel).  Where no
+//     request can be long, a workgroup of a few wavefronts has one request and key head to itself (amap_attend_team_kernel).
 //   Loads: keys, values and the table's entries go straight into LDS (global_load_lds), a ring of two stages, waited for by count.
 //     No wavefront waits for another; while one begins or ends a request its neighbours on the compute unit keep loading.  A token that is not visible is read from 16 bytes of
 //     zeros, so nothing that lies in the cache behind a request's end comes near the sums.
@@ -232,12 +233,237 @@ __device__ __forceinline__ uint32_t sum_up_to(uint32_t x) {   // over the lanes,
     return plus_shifted<0x143, 0xC>(plus_shifted<0x142, 0xA>(x));
 }
 
+// What a lane keeps from segment to segment.
+template <class F>
+struct Lane {
+    uint32_t lane, g, col, base, ids;   // base, ids: of the wavefront's stages in LDS, and of the table's entries behind them
+    // of the 16 bytes that it loads, the row (as an address of ds_bpermute), the piece of it, and both as an offset in half a tile of one page
+    uint32_t row_of[F::LOADS], k_piece[F::LOADS], v_piece[F::LOADS], k_off[F::LOADS], v_off[F::LOADS];
+    uint32_t k_at[2][F::DP / 32], v_at[2][F::DP / 16];   // where its parts of a stage lie
+};
+template <class F>
+__device__ __forceinline__ Lane<F> lane_of(const AttendArgs &a, uint32_t lane, uint32_t base) {
+    const uint32_t g = lane >> 4, col = lane & 15u;
+    Lane<F> w;
+    w.lane = lane, w.g = g, w.col = col, w.base = base, w.ids = base + F::STAGES * F::STAGE;
+#pragma unroll
+    for (int j = 0; j < F::LOADS; ++j) {
+        const uint32_t i = 64u * j + lane, row = i / F::NC, at = i % F::NC;
+        w.row_of[j] = 4u * row;
+        w.k_piece[j] = at ^ key_swizzle<F>(row);
+        w.v_piece[j] = at ^ value_swizzle<F>(row);
+        w.k_off[j] = (((row & 15u) * a.token_step + w.k_piece[j]) << 4) + 4096u - 1024u * (j & 3);
+        w.v_off[j] = (((row & 15u) * a.token_step + w.v_piece[j]) << 4) + 4096u - 1024u * (j & 3);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const uint32_t token = 8u * (col >> 2) + 4u * t + (col & 3u);
+#pragma unroll
+        for (int i = 0; i < F::DP / 32; ++i)
+            w.k_at[t][i] = base + token * F::ROW +
+                         (F::ES == 2 ? ((4u * i + g) ^ key_swizzle<F>(token)) << 4 : (((2u * i + (g >> 1)) ^ key_swizzle<F>(token)) << 4) + ((g & 1u) << 3));
+#pragma unroll
+        for (int i = 0; i < F::DP / 16; ++i) {
+            const uint32_t row = F::ES == 2 ? 8u * g + (col >> 2) + 4u * t : 8u * g + (col >> 1);   // (8-bit: one access, t unused)
+            w.v_at[t][i] = base + F::SIDE + row * F::ROW +
+                         (F::ES == 2 ? ((2u * i + ((col & 3u) >> 1)) ^ value_swizzle<F>(row)) << 4 : ((uint32_t)i ^ value_swizzle<F>(row)) << 4) + ((col & 1u) << 3);
+        }
+    }
+    return w;
+}
+
+// `steps` tiles of a segment from token `begin` on by one wavefront: the results of all its columns, not yet divided (o), a column's largest score less UP
+// (m, in powers of two) and this lane's part of the column's sum of weights (l).
+template <class F>
+__device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Lane<F> &w, uint32_t r, uint32_t kv, uint32_t head0, uint32_t rows, const Seen &seen, uint32_t begin,
+                                             uint32_t steps, f32x4 (&o)[F::DP / 16], float &m, float &l) {
+    typedef typename Of<typename F::T>::eight eight;
+    const uint32_t lane = w.lane, g = w.g, col = w.col, base = w.base, ids = w.ids;
+    const int32_t *const row = a.table + (int64_t)r * a.table_stride;
+    constexpr int LV = F::LOADS, LK = LV + 1;   // loads of a step's values; of its keys and the pages of the step after next
+    auto ask = [&](uint32_t s, uint32_t slot) __attribute__((always_inline)) {   // the pages of step s
+        const uint32_t token = min(max(begin + s * kTokens + (lane & 31u), seen.first), seen.past - 1u);
+        load4(row + fdiv(token, a.by_page), ids + slot * 256u);
+    };
+    uint32_t shown[2];    // of each stage, which tokens are visible
+    uint32_t places = 0;  // of the step being loaded: where this lane's token lies (kNoRow: nowhere), in 16-byte pieces,
+    bool fast = false;    // or, all of them being visible, where either half of them begins
+    int64_t lo = 0, hi = 0;
+    const char *const zeros = reinterpret_cast<const char *>(&kZeros);
+    auto load_side = [&](const char *from, const uint32_t (&off)[F::LOADS], const uint32_t (&piece)[F::LOADS], uint32_t lds) __attribute__((always_inline)) {
+        if (fast) {
+            if (F::PAIRED || a.blocks == 1)
+                load_rows<true>(from + lo, from + hi, off, lds);
+            else
+                load_rows<false>(from + lo, from + hi, off, lds);
+        } else {
+            uint32_t x[F::LOADS];
+#pragma unroll
+            for (int i = 0; i < F::LOADS; ++i) x[i] = (uint32_t)__builtin_amdgcn_ds_bpermute((int)w.row_of[i], (int)places);
+#pragma unroll
+            for (int i = 0; i < F::LOADS; ++i)
+                load16(x[i] != kNoRow && piece[i] < a.pieces ? from + ((uint64_t)(x[i] + piece[i]) << 4) : zeros, lds + 1024u * i);
+        }
+    };
+    auto load_keys = [&](uint32_t s, int slot) __attribute__((always_inline)) {
+        const uint32_t t0 = begin + s * kTokens, token = t0 + (lane & 31u);
+        const uint32_t id = lds_at<uint32_t>(ids + slot * 256u + 4u * (lane & 31u));
+        const bool there = token >= seen.first && token < seen.past && id < a.n_pages;
+        shown[slot] = (uint32_t)__ballot(there);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the keys that were here have been read, and the pages
+        if constexpr (2 * LV + LK + LK > 63) landed<63 - LK>();   // no more than the counter holds
+        fast = F::HALVES && a.halves && shown[slot] == 0xFFFFFFFFu;
+        if (fast) {
+            const uint32_t j0 = fdiv(t0, a.by_page), j1 = fdiv(t0 + 16u, a.by_page), id0 = __builtin_amdgcn_readlane(id, 0), id1 = __builtin_amdgcn_readlane(id, 16);
+            const uint32_t x0 = id0 * a.page_step + (t0 - j0 * a.page) * a.token_step + kv * a.head_step;
+            const uint32_t x1 = id1 * a.page_step + (t0 + 16u - j1 * a.page) * a.token_step + kv * a.head_step;
+            lo = ((int64_t)x0 << 4) - 4096;
+            hi = ((int64_t)x1 << 4) - 4096;
+        } else {
+            const uint32_t j = fdiv(token, a.by_page);
+            places = there ? id * a.page_step + (token - j * a.page) * a.token_step + kv * a.head_step : kNoRow;
+        }
+        load_side(a.k, w.k_off, w.k_piece, base + slot * F::STAGE);
+        ask(s + 2, slot);
+    };
+    auto load_values = [&](int slot) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the values that were here have been read
+        if constexpr (LV + LK + LK + LV > 63) landed<63 - LV>();
+        load_side(a.v, w.v_off, w.v_piece, base + F::SIDE + slot * F::STAGE);
+    };
+#pragma unroll
+    for (int s = 0; s < 2; ++s) ask(s, s);
+    // the queries: column c is query c, or c % 8 where the weights' second parts have columns 8 .. 15
+    eight qf[F::DP / 32];
+    {
+        const uint32_t c = F::PAIRED ? col & 7u : col;
+        const char *const q = a.q + 2 * ((int64_t)r * a.q_token + (int64_t)(head0 + (c < rows ? c : 0u)) * a.q_head);
+#pragma unroll
+        for (int i = 0; i < F::DP / 32; ++i) {
+            const uint32_t d = 32u * i + 8u * g;
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (c < rows && d < a.dim) {
+                if (a.aligned)
+                    x = *reinterpret_cast<const u32x4 *>(q + 2u * d);
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint16_t *const p = reinterpret_cast<const uint16_t *>(q) + d + 2 * e;
+                        x[e] = p[0] | (uint32_t)p[1] << 16;
+                    }
+            }
+            qf[i] = __builtin_bit_cast(eight, x);
+        }
+    }
+    const float by = a.scale * kLog2e * (a.k_scale ? a.k_scale[kv] : 1.f);
+    // (in registers before the first load that is waited for by count: the compiler would wait for them in the loop, each time)
+#pragma unroll
+    for (int i = 0; i < F::DP / 32; ++i) asm volatile("" ::"v"(qf[i]));
+    asm volatile("" ::"v"(by));
+#pragma unroll
+    for (int i = 0; i < F::DP / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+    landed<0>();   // the first pages, and the queries
+    load_keys(0, 0);
+    load_values(0);
+    if (steps > 1) {
+        load_keys(1, 1);
+        load_values(1);
+    }
+    auto step = [&](uint32_t s, auto stage) __attribute__((always_inline)) {
+        constexpr int slot = decltype(stage)::value;
+        const bool next = s + 1 < steps, after = s + 2 < steps;
+        if (next)
+            landed<2 * LV + LK>();
+        else
+            landed<LV>();
+        // ---- scores: this lane's are of column `col` and tokens 8 g .. 8 g + 7
+        f32x4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int i = 0; i < F::DP / 32; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                eight kf;
+                if constexpr (F::ES == 2)
+                    kf = lds_at<eight>(w.k_at[t][i] + slot * F::STAGE);
+                else
+                    kf = eight_of_e4m3<typename F::T>(lds_at<u32x2>(w.k_at[t][i] + slot * F::STAGE));
+                c[t] = Of<typename F::T>::product(kf, qf[i], c[t]);
+            }
+        const uint32_t visible = shown[slot];
+        if (after) load_keys(s + 2, slot);
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = c[j >> 2][j & 3] * by;
+        if (visible != 0xFFFFFFFFu) {
+            const uint32_t mine = visible >> (8u * g);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = mine >> j & 1u ? x[j] : -INFINITY;
+        }
+        float high = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        high = fmaxf(top_of_column(high) - Of<typename F::T>::UP, m);
+        const float from = high == -INFINITY ? 0.f : high;
+        if (__any(high != m)) {
+            const float keep = __builtin_amdgcn_exp2f(m - from);
+            l *= keep;
+#pragma unroll
+            for (int i = 0; i < F::DP / 16; ++i) o[i] *= keep;
+            m = high;
+        }
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(x[j] - from);
+        l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        eight pf, rest;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const typename Of<typename F::T>::one part = (typename Of<typename F::T>::one)p[j];
+            pf[j] = part;
+            rest[j] = (typename Of<typename F::T>::one)(p[j] - (float)part);
+        }
+        if constexpr (F::PAIRED) {
+            if (col >= 8u) pf = rest;
+        }
+        // ---- results: 16 elements of V's rows at a time
+        if (after)
+            landed<2 * LK + LV>();
+        else if (next)
+            landed<LK + LV>();
+        else
+            landed<0>();
+#pragma unroll
+        for (int i = 0; i < F::DP / 16; ++i) {
+            eight vf;
+            if constexpr (F::ES == 2) {
+                union {
+                    i16x4 half[2];
+                    eight whole;
+                } y;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    y.half[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_char *)(uintptr_t)(w.v_at[t][i] + slot * F::STAGE));
+                vf = y.whole;
+            } else {
+                vf = eight_of_e4m3<typename F::T>(__builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(lds_char *)(uintptr_t)(w.v_at[0][i] + slot * F::STAGE))));
+            }
+            o[i] = Of<typename F::T>::product(vf, pf, o[i]);
+            if constexpr (!F::PAIRED) o[i] = Of<typename F::T>::product(vf, rest, o[i]);
+        }
+        if (after) load_values(slot);
+    };
+    for (uint32_t s = 0; s < steps; s += 2) {
+        step(s, std::integral_constant<int, 0>{});
+        if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{});
+    }
+}
+
 template <class F>
 __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(const AttendArgs a) {
-    typedef typename Of<typename F::T>::eight eight;
     extern __shared__ char smem[];
     const uint32_t lane = threadIdx.x, g = lane >> 4, col = lane & 15u;
-    const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)smem, ids = base + F::STAGES * F::STAGE;
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_char *)smem;
 
     // (the arguments that come later too: another wait for them costs 0.3 us)
     asm volatile("" ::"s"(a.k), "s"(a.v), "s"(a.q), "s"(a.out), "s"(a.lse), "s"(a.parts), "s"(a.splits), "s"(a.k_scale), "s"(a.table), "s"(a.table_stride), "s"(a.scale), "s"(a.by_page.mul),
@@ -302,35 +528,7 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
     Seen seen = seen_of(a, length);
     uint32_t segment = (u - first_of) / seen.units, at = u - first_of - segment * seen.units;   // `at`: of the segment's units
 
-    // ---- what does not change from segment to segment: of the 16 bytes that this lane loads, the row (as an address of ds_bpermute), the piece of
-    // it, and both as an offset in half a tile of one page
-    uint32_t row_of[F::LOADS], k_piece[F::LOADS], v_piece[F::LOADS], k_off[F::LOADS], v_off[F::LOADS];
-#pragma unroll
-    for (int j = 0; j < F::LOADS; ++j) {
-        const uint32_t i = 64u * j + lane, row = i / F::NC, at = i % F::NC;
-        row_of[j] = 4u * row;
-        k_piece[j] = at ^ key_swizzle<F>(row);
-        v_piece[j] = at ^ value_swizzle<F>(row);
-        k_off[j] = (((row & 15u) * a.token_step + k_piece[j]) << 4) + 4096u - 1024u * (j & 3);
-        v_off[j] = (((row & 15u) * a.token_step + v_piece[j]) << 4) + 4096u - 1024u * (j & 3);
-    }
-    // where this lane's parts of a stage lie
-    uint32_t k_at[2][F::DP / 32], v_at[2][F::DP / 16];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const uint32_t token = 8u * (col >> 2) + 4u * t + (col & 3u);
-#pragma unroll
-        for (int i = 0; i < F::DP / 32; ++i)
-            k_at[t][i] = base + token * F::ROW +
-                         (F::ES == 2 ? ((4u * i + g) ^ key_swizzle<F>(token)) << 4 : (((2u * i + (g >> 1)) ^ key_swizzle<F>(token)) << 4) + ((g & 1u) << 3));
-#pragma unroll
-        for (int i = 0; i < F::DP / 16; ++i) {
-            const uint32_t row = F::ES == 2 ? 8u * g + (col >> 2) + 4u * t : 8u * g + (col >> 1);   // (8-bit: one access, t unused)
-            v_at[t][i] = base + F::SIDE + row * F::ROW +
-                         (F::ES == 2 ? ((2u * i + ((col & 3u) >> 1)) ^ value_swizzle<F>(row)) << 4 : ((uint32_t)i ^ value_swizzle<F>(row)) << 4) + ((col & 1u) << 3);
-        }
-    }
-
+    const Lane<F> w = lane_of<F>(a, lane, base);
     while (u < end) {
         // the piece of this segment in the share: its tiles follow the units of its beginning
         const uint32_t past = min(seen.units, at + (end - u)), tile = at > kBegin ? at - kBegin : 0u, n = past > kBegin ? past - kBegin - tile : 0u;
@@ -339,185 +537,9 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
         const uint32_t q0 = block * a.columns, rows = min(a.group - q0, a.columns);   // queries of the block
         const uint32_t head0 = kv * a.group + q0;
 
-        const uint32_t begin = (seen.tile + tile) * kTokens, steps = n;
-        const int32_t *const row = a.table + (int64_t)r * a.table_stride;
-        constexpr int LV = F::LOADS, LK = LV + 1;   // loads of a step's values; of its keys and the pages of the step after next
-        auto ask = [&](uint32_t s, uint32_t slot) __attribute__((always_inline)) {   // the pages of step s
-            const uint32_t token = min(max(begin + s * kTokens + (lane & 31u), seen.first), seen.past - 1u);
-            load4(row + fdiv(token, a.by_page), ids + slot * 256u);
-        };
-        uint32_t shown[2];    // of each stage, which tokens are visible
-        uint32_t places = 0;  // of the step being loaded: where this lane's token lies (kNoRow: nowhere), in 16-byte pieces,
-        bool fast = false;    // or, all of them being visible, where either half of them begins
-        int64_t lo = 0, hi = 0;
-        const char *const zeros = reinterpret_cast<const char *>(&kZeros);
-        auto load_side = [&](const char *from, const uint32_t (&off)[F::LOADS], const uint32_t (&piece)[F::LOADS], uint32_t lds) __attribute__((always_inline)) {
-            if (fast) {
-                if (F::PAIRED || a.blocks == 1)
-                    load_rows<true>(from + lo, from + hi, off, lds);
-                else
-                    load_rows<false>(from + lo, from + hi, off, lds);
-            } else {
-                uint32_t x[F::LOADS];
-#pragma unroll
-                for (int i = 0; i < F::LOADS; ++i) x[i] = (uint32_t)__builtin_amdgcn_ds_bpermute((int)row_of[i], (int)places);
-#pragma unroll
-                for (int i = 0; i < F::LOADS; ++i)
-                    load16(x[i] != kNoRow && piece[i] < a.pieces ? from + ((uint64_t)(x[i] + piece[i]) << 4) : zeros, lds + 1024u * i);
-            }
-        };
-        auto load_keys = [&](uint32_t s, int slot) __attribute__((always_inline)) {
-            const uint32_t t0 = begin + s * kTokens, token = t0 + (lane & 31u);
-            const uint32_t id = lds_at<uint32_t>(ids + slot * 256u + 4u * (lane & 31u));
-            const bool there = token >= seen.first && token < seen.past && id < a.n_pages;
-            shown[slot] = (uint32_t)__ballot(there);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the keys that were here have been read, and the pages
-            if constexpr (2 * LV + LK + LK > 63) landed<63 - LK>();   // no more than the counter holds
-            fast = F::HALVES && a.halves && shown[slot] == 0xFFFFFFFFu;
-            if (fast) {
-                const uint32_t j0 = fdiv(t0, a.by_page), j1 = fdiv(t0 + 16u, a.by_page), id0 = __builtin_amdgcn_readlane(id, 0), id1 = __builtin_amdgcn_readlane(id, 16);
-                const uint32_t x0 = id0 * a.page_step + (t0 - j0 * a.page) * a.token_step + kv * a.head_step;
-                const uint32_t x1 = id1 * a.page_step + (t0 + 16u - j1 * a.page) * a.token_step + kv * a.head_step;
-                lo = ((int64_t)x0 << 4) - 4096;
-                hi = ((int64_t)x1 << 4) - 4096;
-            } else {
-                const uint32_t j = fdiv(token, a.by_page);
-                places = there ? id * a.page_step + (token - j * a.page) * a.token_step + kv * a.head_step : kNoRow;
-            }
-            load_side(a.k, k_off, k_piece, base + slot * F::STAGE);
-            ask(s + 2, slot);
-        };
-        auto load_values = [&](int slot) __attribute__((always_inline)) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the values that were here have been read
-            if constexpr (LV + LK + LK + LV > 63) landed<63 - LV>();
-            load_side(a.v, v_off, v_piece, base + F::SIDE + slot * F::STAGE);
-        };
-#pragma unroll
-        for (int s = 0; s < 2; ++s) ask(s, s);
-        // the queries: column c is query c, or c % 8 where the weights' second parts have columns 8 .. 15
-        eight qf[F::DP / 32];
-        {
-            const uint32_t c = F::PAIRED ? col & 7u : col;
-            const char *const q = a.q + 2 * ((int64_t)r * a.q_token + (int64_t)(head0 + (c < rows ? c : 0u)) * a.q_head);
-#pragma unroll
-            for (int i = 0; i < F::DP / 32; ++i) {
-                const uint32_t d = 32u * i + 8u * g;
-                u32x4 x = {0u, 0u, 0u, 0u};
-                if (c < rows && d < a.dim) {
-                    if (a.aligned)
-                        x = *reinterpret_cast<const u32x4 *>(q + 2u * d);
-                    else
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint16_t *const p = reinterpret_cast<const uint16_t *>(q) + d + 2 * e;
-                            x[e] = p[0] | (uint32_t)p[1] << 16;
-                        }
-                }
-                qf[i] = __builtin_bit_cast(eight, x);
-            }
-        }
-        const float by = a.scale * kLog2e * (a.k_scale ? a.k_scale[kv] : 1.f);
-        // (in registers before the first load that is waited for by count: the compiler would wait for them in the loop, each time)
-#pragma unroll
-        for (int i = 0; i < F::DP / 32; ++i) asm volatile("" ::"v"(qf[i]));
-        asm volatile("" ::"v"(by));
         f32x4 o[F::DP / 16];
-#pragma unroll
-        for (int i = 0; i < F::DP / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;   // m: the largest score less UP
-        landed<0>();   // the first pages, and the queries
-        load_keys(0, 0);
-        load_values(0);
-        if (steps > 1) {
-            load_keys(1, 1);
-            load_values(1);
-        }
-        auto step = [&](uint32_t s, auto stage) __attribute__((always_inline)) {
-            constexpr int slot = decltype(stage)::value;
-            const bool next = s + 1 < steps, after = s + 2 < steps;
-            if (next)
-                landed<2 * LV + LK>();
-            else
-                landed<LV>();
-            // ---- scores: this lane's are of column `col` and tokens 8 g .. 8 g + 7
-            f32x4 c[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-            for (int i = 0; i < F::DP / 32; ++i)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    eight kf;
-                    if constexpr (F::ES == 2)
-                        kf = lds_at<eight>(k_at[t][i] + slot * F::STAGE);
-                    else
-                        kf = eight_of_e4m3<typename F::T>(lds_at<u32x2>(k_at[t][i] + slot * F::STAGE));
-                    c[t] = Of<typename F::T>::product(kf, qf[i], c[t]);
-                }
-            const uint32_t visible = shown[slot];
-            if (after) load_keys(s + 2, slot);
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = c[j >> 2][j & 3] * by;
-            if (visible != 0xFFFFFFFFu) {
-                const uint32_t mine = visible >> (8u * g);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = mine >> j & 1u ? x[j] : -INFINITY;
-            }
-            float high = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            high = fmaxf(top_of_column(high) - Of<typename F::T>::UP, m);
-            const float from = high == -INFINITY ? 0.f : high;
-            if (__any(high != m)) {
-                const float keep = __builtin_amdgcn_exp2f(m - from);
-                l *= keep;
-#pragma unroll
-                for (int i = 0; i < F::DP / 16; ++i) o[i] *= keep;
-                m = high;
-            }
-            float p[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(x[j] - from);
-            l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-            eight pf, rest;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const typename Of<typename F::T>::one part = (typename Of<typename F::T>::one)p[j];
-                pf[j] = part;
-                rest[j] = (typename Of<typename F::T>::one)(p[j] - (float)part);
-            }
-            if constexpr (F::PAIRED) {
-                if (col >= 8u) pf = rest;
-            }
-            // ---- results: 16 elements of V's rows at a time
-            if (after)
-                landed<2 * LK + LV>();
-            else if (next)
-                landed<LK + LV>();
-            else
-                landed<0>();
-#pragma unroll
-            for (int i = 0; i < F::DP / 16; ++i) {
-                eight vf;
-                if constexpr (F::ES == 2) {
-                    union {
-                        i16x4 half[2];
-                        eight whole;
-                    } y;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        y.half[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_char *)(uintptr_t)(v_at[t][i] + slot * F::STAGE));
-                    vf = y.whole;
-                } else {
-                    vf = eight_of_e4m3<typename F::T>(__builtin_bit_cast(
-                        u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(lds_char *)(uintptr_t)(v_at[0][i] + slot * F::STAGE))));
-                }
-                o[i] = Of<typename F::T>::product(vf, pf, o[i]);
-                if constexpr (!F::PAIRED) o[i] = Of<typename F::T>::product(vf, rest, o[i]);
-            }
-            if (after) load_values(slot);
-        };
-        for (uint32_t s = 0; s < steps; s += 2) {
-            step(s, std::integral_constant<int, 0>{});
-            if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{});
-        }
+        float m, l;
+        attend_tiles<F>(a, w, r, kv, head0, rows, seen, (seen.tile + tile) * kTokens, n, o, m, l);
 
         // ---- the results, through LDS (in the place of the stages) into rows; a piece of a segment into the workspace
         l = sum_of_column(l);
@@ -629,6 +651,59 @@ __global__ __launch_bounds__(THREADS) void amap_attend_join_kernel(const JoinArg
     }
 }
 
+// One segment to a workgroup, its tiles dealt to the wavefronts, which join what they have through LDS: one launch and no workspace, for calls whose
+// segments are all short (team_of says which).
+template <class F>
+__global__ __launch_bounds__(64 * F::PER_UNIT, (F::PER_UNIT + 3) / 4) void amap_attend_team_kernel(const AttendArgs a) {
+    typedef typename Of<typename F::T>::one one;
+    extern __shared__ char smem[];
+    const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const uint32_t stages = (uint32_t)(uintptr_t)(lds_char *)smem;
+    const uint32_t r = fdiv(blockIdx.x, a.by_segments), segment = blockIdx.x - r * a.segments;
+    const uint32_t kv = fdiv(segment, a.by_blocks), q0 = (segment - kv * a.blocks) * a.columns, rows = min(a.group - q0, a.columns), head0 = kv * a.group + q0;
+    const Seen seen = seen_of(a, a.length[r]);
+    const uint32_t each = (seen.tiles + waves - 1) / waves, first = wave * each, n = first < seen.tiles ? min(each, seen.tiles - first) : 0u;
+    const uint32_t base = stages + wave * F::LDS, stats = F::STAGES * F::STAGE;   // stats: of a wavefront's LDS, maxima and sums of its columns
+    if (n) {
+        const Lane<F> w = lane_of<F>(a, lane, base);
+        f32x4 o[F::DP / 16];
+        float m, l;
+        attend_tiles<F>(a, w, r, kv, head0, rows, seen, (seen.tile + first) * kTokens, n, o, m, l);
+        l = sum_of_column(l);
+#pragma unroll
+        for (int i = 0; i < F::DP / 16; ++i) lds_put<f32x4>(base + 4u * (w.col * F::OUT_ROW + 16u * i + 4u * w.g), o[i]);
+        if (lane < kColumns) {
+            lds_put<float>(base + stats + 4u * lane, m);
+            lds_put<float>(base + stats + 64u + 4u * lane, l);
+        }
+    }
+    __syncthreads();
+    const uint32_t parts = each ? (seen.tiles + each - 1) / each : 0u;   // wavefronts that had something
+    const float vs = a.v_scale ? a.v_scale[kv] : 1.f;
+    for (uint32_t i = threadIdx.x; i < rows * (F::DP / 4); i += blockDim.x) {
+        const uint32_t c = i / (F::DP / 4), d = 4u * (i % (F::DP / 4));
+        float high = -INFINITY, sum = 0.f;
+        for (uint32_t p = 0; p < parts; ++p) high = fmaxf(high, lds_at<float>(stages + p * F::LDS + stats + 4u * c));
+        const float from = high == -INFINITY ? 0.f : high;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t p = 0; p < parts; ++p) {
+            const uint32_t at = stages + p * F::LDS;
+            const float take = __builtin_amdgcn_exp2f(lds_at<float>(at + stats + 4u * c) - from);
+            sum += take * lds_at<float>(at + stats + 64u + 4u * c);
+            f32x4 y = lds_at<f32x4>(at + 4u * (c * F::OUT_ROW + d));
+            if constexpr (F::PAIRED) y += lds_at<f32x4>(at + 4u * ((c + 8u) * F::OUT_ROW + d));
+            x += y * take;
+        }
+        const bool none = sum == 0.f;   // (nothing seen, or scores of -inf only)
+        const float by = none ? 0.f : vs / sum;
+        one *const out = reinterpret_cast<one *>(a.out) + (int64_t)r * a.out_token + (int64_t)(head0 + c) * a.out_head + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (d + e < a.dim) out[e] = (one)(none ? 0.f : x[e] * by);
+        if (d == 0 && a.lse) a.lse[(int64_t)r * a.heads + head0 + c] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+}
+
 // How a call is cut: workgroups, columns of a block, and whether a segment may be split between workgroups.
 struct Cut {
     uint32_t groups, columns, blocks, segments;
@@ -638,7 +713,16 @@ struct Cut {
 };
 
 template <class F>
-amap_status attend(AttendArgs a, const Cut &cut, hipStream_t s) {
+amap_status attend(AttendArgs a, const Cut &cut, uint32_t team, hipStream_t s) {
+    if (team) {
+        if constexpr (F::PER_UNIT * F::LDS > 65536) {
+            static LdsReservation reserved;
+            const hipError_t e = reserved.on_current_device({reinterpret_cast<const void *>(amap_attend_team_kernel<F>)}, F::PER_UNIT * F::LDS);
+            if (e != hipSuccess) return launched(e, "amap_attend_team_kernel: cannot reserve its LDS stages");
+        }
+        const hipError_t e = launch_kernel<amap_attend_team_kernel<F>>(dim3(a.requests * a.segments), dim3(64u * team), team * F::LDS, s, a);
+        return launched(e, "amap_attend_team_kernel");
+    }
     if constexpr (F::LDS > 65536) {
         static LdsReservation reserved;
         const hipError_t e = reserved.on_current_device({reinterpret_cast<const void *>(amap_attend_kernel<F>)}, F::LDS);
@@ -713,6 +797,32 @@ amap_status cut_of(const amap_cache &c, int heads, int64_t requests, int table_w
     cut.parts = (requests * cut.segments * (int64_t)sizeof(Split) + 15) / 16 * 16;
     cut.bytes = cut.splits ? cut.parts + (int64_t)cut.groups * (2 * 4 * kColumns * (cut.dp + 2)) : 0;
     return AMAP_OK;
+}
+
+// Wavefronts of a workgroup that has a segment to itself, or 0 for shares.  A compute unit by itself loads 52 bytes a ns, by four wavefronts as by eight (2000 tokens of 64,
+// one, two, four, eight of them: 44, 24.6, 15.1, 15.5 us), and the join of shares costs 4 to 6 us: so segments up to 288 KB (16 requests of 500 tokens, heads of 128, four to
+// a key head: 14.0 -> 11.0 us; four of 1000 tokens 12.4 by shares and 15.5), and 512 KB where all compute units have one (a window of 1000, 256 requests, heads of 96: 18.9 -> 13.3).  No more wavefronts
+// than the chip holds at once (1600 segments of 500 tokens, one, two, three, four of them: 16.3, 14.7, 15.4, 17.7), and none with less than 32 KB.  A wavefront's
+// own part: up to 96 KB and 10 tiles (8 tiles of heads of 256, 32 KB each, by two wavefronts: 14.2 us, by shares 12.7).
+template <class F>
+uint32_t team_of(const AttendArgs &a) {
+    uint32_t tiles = (a.most + kTokens - 1) / kTokens;   // of the longest segment that the table and the window allow: lengths are on the device
+    if (a.window) {
+        const uint32_t seen = (a.window - 1) / kTokens + 2;   // tiles that a window can touch
+        tiles = tiles < seen ? tiles : seen;
+    }
+    if (tiles < 2) return 1;
+    constexpr uint32_t kSteps = at_most(10, 98304 / F::STAGE);
+    const uint64_t segments = (uint64_t)a.requests * a.segments, bytes = (uint64_t)tiles * F::STAGE;
+    if (bytes > (segments < kUnits ? 288u << 10 : 512u << 10)) return 0;
+    uint64_t most = (kUnits * F::PER_UNIT + segments - 1) / segments;
+    if (most > F::PER_UNIT) most = F::PER_UNIT;
+    uint64_t waves = (bytes + 32767) / 32768;
+    if (waves > 4) waves = 4;
+    if (waves * kSteps < tiles) waves = (tiles + kSteps - 1) / kSteps;
+    if (waves > most) waves = most;
+    const uint32_t steps = (uint32_t)((tiles + waves - 1) / waves);
+    return steps <= kSteps ? (tiles + steps - 1) / steps : 0u;
 }
 
 }  // namespace
@@ -797,6 +907,6 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     // (16 rows of a page within 32-bit byte offsets; heads of a whole form: no pieces of zeros)
     a.halves = cache->page_size % 16 == 0 && dim == cut.dp && (cache->page_size == 1 || cache->token_stride * es * 16 < ((int64_t)1 << 31));
     a.scale = scale;
-    with_form(q->type, cache->type, cut.dp, cut.columns == 8, [&](auto form) { st = attend<decltype(form)>(a, cut, s); });
+    with_form(q->type, cache->type, cut.dp, cut.columns == 8, [&](auto form) { st = attend<decltype(form)>(a, cut, team_of<decltype(form)>(a), s); });
     return st;
 }

@@ -304,6 +304,27 @@ def test_attend(dev, lengths, heads, kv, dim, page, dtype, to, order, window):
     _check(got, _expect(cache, q, table, length, dim ** -0.5, window), q, max(lengths))
 
 
+@pytest.mark.parametrize("lengths, heads, kv, dim, page, dtype, to, order, window", [c for c in ATTEND if max(c[0]) < 5000])
+def test_attend_of_a_wide_table(dev, lengths, heads, kv, dim, page, dtype, to, order, window):
+    """The same requests in a table that has room for long ones: other workgroups, the same result but for roundings."""
+    cache, q, table, length = _requests(dev, sum(lengths) + dim, lengths, heads, kv, dim, page, dtype, to, order, window=window)
+    wide = torch.full((len(lengths), -(-40000 // page)), -1, dtype=torch.int32)
+    wide[:, :table.size(1)] = table
+    got = dev.cache_attend(cache, q, wide.cuda(), length.cuda(), window=window)
+    _check(got, _expect(cache, q, table, length, dim ** -0.5, window), q, max(lengths))
+
+
+@pytest.mark.parametrize("requests, heads, kv, dim, dtype, to", [
+    (300, 8, 8, 64, BF16, BF16), (40, 16, 2, 96, F16, F16), (150, 4, 4, 128, BF16, BF16), (2, 64, 2, 256, F16, F16), (37, 24, 1, 128, BF16, E4M3), (5, 3, 3, 256, F16, E4M3),
+])
+@pytest.mark.parametrize("longest", [31, 100, 300])
+def test_attend_by_size(dev, requests, heads, kv, dim, dtype, to, longest):
+    """From one wavefront to a segment to as many as a compute unit holds."""
+    lengths = [int(v) for v in np.random.default_rng(longest + dim).integers(0, longest + 1, requests)] + [longest]
+    cache, q, table, length = _requests(dev, longest, lengths, heads, kv, dim, 16, dtype, to, "tokens")
+    _check(dev.cache_attend(cache, q, table.cuda(), length.cuda()), _expect(cache, q, table, length, dim ** -0.5), q, longest)
+
+
 def test_attend_many_short_requests(dev):
     lengths = [int(v) for v in np.random.default_rng(5).integers(0, 90, 700)]
     cache, q, table, length = _requests(dev, 8, lengths, 4, 2, 64, 16, BF16, BF16, "tokens")
