@@ -471,7 +471,7 @@ typedef struct {
  * far as the table is wide; the table's other entries are neither read nor written but those of pages that fresh tokens go on in.  The
  * step's tokens, request after request, get their owner, position cached + i and slot; a token without a page (the list or
  * the table's row at its end, or an entry that is no page: < 0) gets slot -1, and everything from the last token
- * to n_tokens -1.  All arrays are int32 but slot.  `cached` and `table` may be read again: the same call gives the same.
+ * to n_tokens -1.  All arrays are int32 but slot, and none that is written overlaps another.  `cached` and `table` may be read again: the same call gives the same.
  * requests <= 16384; sums of tokens under 2^31.  Negative lengths count as 0. */
 typedef struct {
     int64_t requests;

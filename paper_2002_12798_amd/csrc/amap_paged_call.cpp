@@ -128,9 +128,9 @@ struct Making {
 };
 at::Tensor made(at::IntArrayRef size, const at::Tensor &beside, at::ScalarType type) { return at::empty(size, beside.options().dtype(type).requires_grad(false)); }
 
-// `size` words of a buffer from word `at` on, as a view of it (through the dispatcher 0.4 us each)
-at::Tensor part(const at::Tensor &words, int64_t size, int64_t at) {
-    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(words.storage()), words.key_set(), words.dtype());
+// `size` elements of a type in a buffer, from its element `at` of that type on, as a view of it (through the dispatcher 0.4 us each)
+at::Tensor part(const at::Tensor &buffer, at::ScalarType type, int64_t size, int64_t at) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(buffer.storage()), buffer.key_set(), c10::scalarTypeToTypeMeta(type));
     t.unsafeGetTensorImpl()->set_storage_offset(at);
     t.unsafeGetTensorImpl()->set_sizes_contiguous({size});
     return t;
@@ -282,17 +282,19 @@ PyObject *assign(PyObject *const *a, Py_ssize_t n) {
         out.o = again(a[6]);
     } else {
         Making without;
-        const at::Tensor words = made({2 * requests + 2 + 2 * tokens}, *tf, at::kInt);
-        Ref whole_of(PyTuple_New(6));
-        if (!whole_of.o) return nullptr;
-        int64_t at = 0;
-        for (const int i : {0, 1, 3, 4, 5, 2}) {
-            PyObject *const o = THPVariable_Wrap(i == 2 ? made({tokens}, *tf, at::kLong) : part(words, size[i], at));
+        const at::Tensor words = made({2 * requests + 2 + 4 * tokens}, *tf, at::kInt);   // (one buffer: the slots first, 8 bytes each)
+        Ref all(PyTuple_New(6));
+        if (!all.o) return nullptr;
+        int64_t at = 2 * tokens;
+        for (int i = 0; i < 6; ++i) {
+            PyObject *const o = THPVariable_Wrap(i == 2 ? part(words, at::kLong, tokens, 0) : part(words, at::kInt, size[i], at));
             if (!o) return nullptr;
-            PyTuple_SET_ITEM(whole_of.o, i, o);
-            at += size[i];
+            PyTuple_SET_ITEM(all.o, i, o);
+            at += i == 2 ? 0 : size[i];
         }
-        out.o = PyObject_Call(assigned, whole_of.o, nullptr);
+        // (a named tuple's own constructor is a Python function that does this)
+        Ref args(PyTuple_Pack(1, all.o));
+        out.o = args.o ? PyTuple_Type.tp_new(reinterpret_cast<PyTypeObject *>(assigned), args.o, nullptr) : nullptr;
         if (!out.o || !PyTuple_Check(out.o)) return nullptr;
     }
     amap_assign g = {};
@@ -336,7 +338,7 @@ PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // device, current device, whether CUDA is initialised, whether the current stream is being captured)
 PyObject *library(PyObject *, PyObject *const *a, Py_ssize_t n) {
     void *p[5];
-    bool ok = n == 10;
+    bool ok = n == 10 && PyType_Check(a[5]) && PyType_IsSubtype(reinterpret_cast<PyTypeObject *>(a[5]), &PyTuple_Type);
     for (int i = 0; ok && i < 5; ++i) ok = address(a[i], &p[i]);
     if (!ok) {
         PyErr_SetString(PyExc_TypeError, "five addresses, a type and four functions");

@@ -210,9 +210,9 @@ class Assigned(NamedTuple):
 def assigned_buffers(requests, n_tokens, like=None) -> Assigned:
     """Room for a step's assignment, for a program that keeps it from step to step (as a captured graph has to)."""
     dev = require_gpu() if like is None else like.device
-    words = torch.empty(2 * requests + 2 + 2 * n_tokens, dtype=torch.int32, device=dev)
-    begin, length, position, owner, taken = words.split_with_sizes((requests + 1, requests, n_tokens, n_tokens, 1))
-    return Assigned(begin, length, torch.empty(n_tokens, dtype=torch.int64, device=dev), position, owner, taken)
+    words = torch.empty(2 * requests + 2 + 4 * n_tokens, dtype=torch.int32, device=dev)
+    slot, begin, length, position, owner, taken = words.split_with_sizes((2 * n_tokens, requests + 1, requests, n_tokens, n_tokens, 1))
+    return Assigned(begin, length, slot.view(torch.int64), position, owner, taken)
 
 
 class _NoCalls:

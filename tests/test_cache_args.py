@@ -49,6 +49,18 @@ def test_assign(over, status):
     assert status != B.AMAP_E_UNSUPPORTED or "16384" in said
 
 
+def test_assign_to_arrays_that_overlap():
+    """4 requests, 9 free pages, 32 tokens, a table of 4 rows of 8: every array a page apart, then one of those written within another."""
+    names = ["cached", "fresh", "free_pages", "table", "begin", "length", "slot", "position", "owner", "taken"]
+    size = dict(cached=16, fresh=16, free_pages=36, table=128, begin=20, length=16, slot=256, position=128, owner=128, taken=4)
+    at = {n: AT + 4096 * i for i, n in enumerate(names)}
+    for i, n in enumerate(names[3:]):
+        for m in names:
+            if m != n:
+                _refuses(B.AMAP_E_ALIAS, B.amap_cache_assign, _assign(**{**at, n: at[m] + size[m] - 4}))
+                _refuses(B.AMAP_E_ALIAS, B.amap_cache_assign, _assign(**{**at, n: at[m] - size[n] + 4}))
+
+
 @pytest.mark.parametrize("x, out, dim, rope, position, status", [
     (_rows(), _rows(5 * AT), 64, _rope(33, (33,)), AT, B.AMAP_E_SHAPE),                       # more pairs than halves
     (_rows(), _rows(5 * AT), 64, _rope(32, (16, 15)), AT, B.AMAP_E_SHAPE),                    # axes that do not add up
