@@ -114,6 +114,30 @@ def test_both_ways_give_the_same(monkeypatch):
 
 
 @pytest.mark.gpu
+def test_outputs_of_one_allocation():
+    """What a call makes is as a user would make it: contiguous, of its own type, apart, without a gradient; odd sizes, no requests and no tokens among them."""
+    k, v = (torch.randn((8, 16, 3, 40)).half().cuda() for _ in range(2))
+    cache = device.PagedCache(k, v)
+    for n in (0, 1, 3):
+        q = torch.randn((n, 3, 40)).half().cuda().requires_grad_()
+        table, length = torch.arange(2 * n, dtype=torch.int32, device="cuda").view(n, 2), torch.full((n,), 20, dtype=torch.int32, device="cuda")
+        out, lse = device.cache_attend(cache, q, table, length)
+        given = torch.empty_like(out), torch.empty((n, 3), device="cuda")
+        device.cache_attend(cache, q, table, length, out=given[0], lse=given[1])
+        for got, want in zip((out, lse), given):
+            assert got.shape == want.shape and got.dtype == want.dtype and got.is_contiguous() and not got.requires_grad and torch.equal(got, want)
+        before = lse.clone()
+        out.zero_()
+        assert torch.equal(lse, before)
+    fresh, free = torch.tensor([3, 0], dtype=torch.int32, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda")
+    for tokens in (0, 3, 5):
+        a = device.cache_assign(2, None, fresh, torch.full((2, 2), -1, dtype=torch.int32, device="cuda"), free, tokens)
+        assert type(a) is device.Assigned and all(t.is_contiguous() for t in a) and a.slot.dtype == torch.int64
+        assert a.begin.tolist() == [0, 3, 3] and a.length.tolist() == [3, 0] and a.taken.tolist() == [2]
+        assert a.slot.tolist() == [0, 1, 2, -1, -1][:tokens] and a.position.tolist() == [0, 1, 2, -1, -1][:tokens] and a.owner.tolist() == [0, 0, 0, -1, -1][:tokens]
+
+
+@pytest.mark.gpu
 def test_the_workspace_that_a_cache_keeps():
     """One for each stream that it was called on, grown when a call needs more, none made while a graph is captured."""
     k, v = (torch.randn((64, 16, 1, 64)).bfloat16().cuda() for _ in range(2))
