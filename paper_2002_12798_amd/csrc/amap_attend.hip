@@ -16,6 +16,8 @@
 //   A weight is kept in two 16-bit parts, itself rounded and what that leaves: one part alone would be off by as much as
 //     the result's own rounding is.  With up to 8 queries to a key head the second part costs nothing: it takes the columns that are
 //     idle.  (A value that is infinite makes its column NaN, as 0 * inf does in the sum itself where a weight has vanished.)
+// Measured, cold: two requests of 131072 tokens, 32 queries to 8 key heads of 128, bf16 (1.07 GB) 181 us, 5.9 TB/s; 64 ragged ones up to 4096 (140 MB) 33.5 us, 28 of
+// them over shares and 5 of joining; 128 up to 2048 of an 8-bit cache, 12 heads of 64 (54 MB) 19 us; one of 500, 16 heads of 64, 6.5 us.
 #include "amap_cache.hpp"
 
 #include <type_traits>
@@ -30,7 +32,9 @@ constexpr uint32_t kUnits = 256;   // compute units of an MI355X
 constexpr int kTokens = 32;        // of a wavefront's step
 constexpr int kColumns = 16;       // queries of a workgroup at a time (8 where their weights' second parts have the others)
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
-constexpr uint32_t kBegin = 3;             // what beginning and ending a segment counts for in a share, in tiles
+// What beginning and ending a segment counts for in a share, in tiles (1, 3, 6, 10 of them: 16 requests of about 1500 tokens 26.2 us by 3 and 27 by 10, 128 ragged ones of an 8-bit
+// cache 20.2 and 22.2; 6 level with 3).
+constexpr uint32_t kBegin = 3;
 constexpr uint32_t kMostJoining = 8192;    // workgroups of a join
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
@@ -811,9 +815,11 @@ uint32_t team_of(const AttendArgs &a) {
         const uint32_t seen = (a.window - 1) / kTokens + 2;   // tiles that a window can touch
         tiles = tiles < seen ? tiles : seen;
     }
+    const uint64_t segments = (uint64_t)a.requests * a.segments;
+    if (segments > 1u << 22) return 0;   // (a launch counts its threads in 32 bits)
     if (tiles < 2) return 1;
     constexpr uint32_t kSteps = at_most(10, 98304 / F::STAGE);
-    const uint64_t segments = (uint64_t)a.requests * a.segments, bytes = (uint64_t)tiles * F::STAGE;
+    const uint64_t bytes = (uint64_t)tiles * F::STAGE;
     if (bytes > (segments < kUnits ? 288u << 10 : 512u << 10)) return 0;
     uint64_t most = (kUnits * F::PER_UNIT + segments - 1) / segments;
     if (most > F::PER_UNIT) most = F::PER_UNIT;

