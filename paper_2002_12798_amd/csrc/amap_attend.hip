@@ -32,7 +32,7 @@ constexpr uint32_t kUnits = 256;   // compute units of an MI355X
 constexpr int kTokens = 32;        // of a wavefront's step
 constexpr int kColumns = 16;       // queries of a workgroup at a time (8 where their weights' second parts have the others)
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
-// What beginning and ending a segment counts for in a share, in tiles (1, 3, 6, 10 of them: 16 requests of about 1500 tokens 26.2 us by 3 and 27 by 10, 128 ragged ones of an 8-bit
+// What beginning and ending a segment counts for in a share, in tiles (1, 3, 6 or 10: 16 requests of about 1500 tokens 26.2 us by 3 and 27 by 10, 128 ragged ones of an 8-bit
 // cache 20.2 and 22.2; 6 level with 3).
 constexpr uint32_t kBegin = 3;
 constexpr uint32_t kMostJoining = 8192;    // workgroups of a join
