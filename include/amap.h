@@ -509,7 +509,8 @@ amap_status amap_cache_append(const amap_cache *cache, const amap_heads *k, cons
  * by row.  A row that sees no token, or whose scores are all -inf, is 0 with lse -inf.  Heads heads / kv_heads * h .. share key head h.  What lies in
  * the cache outside the visible tokens is never used, whatever it holds.  A length beyond the table's width counts as
  * that.  q and out: BF16 or F16 alike; head_dim a multiple of 8 (E4M3: 16) up to 256, rows of the cache 16-byte aligned.
- * workspace: amap_cache_attend_workspace bytes, 16-byte aligned; its contents need not be kept. */
+ * workspace: amap_cache_attend_workspace bytes, 16-byte aligned; its contents need not be kept.  A call issues up to two launches, and the second reads
+ * what the first left there: two calls may have the same workspace only if all launches of one are on the stream before the other is called. */
 amap_status amap_cache_attend(const amap_cache *cache, const amap_heads *q, int64_t requests, const int32_t *table, int64_t table_stride,
                               int table_width, const int32_t *length, float scale, int window, const amap_heads *out, float *lse,
                               void *workspace, int64_t workspace_bytes, void *stream);

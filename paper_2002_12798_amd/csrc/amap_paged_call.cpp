@@ -217,6 +217,33 @@ PyObject *append(PyObject *const *a, Py_ssize_t n) {
                   again(turned ? out.o : Py_True));
 }
 
+// The workspace that a cache keeps for a stream, taken out of its dictionary for as long as a call issues its launches (they let other Python threads run)
+// and put back behind them: a call of another thread finds none in the meantime and has one of its own, so no two calls whose launches may come one between
+// the other's share one.  (Once both are on the stream, whichever was put back last is what the next call finds.)
+struct Kept {
+    Ref all, key, room;
+    bool taken = false;
+    // what is there, if it is large enough
+    const at::Tensor *look(PyObject *cache, void *stream, int64_t need) {
+        all.o = PyObject_GetAttr(cache, s_work);
+        key.o = all.o ? PyLong_FromVoidPtr(stream) : nullptr;
+        PyObject *const o = key.o && PyDict_CheckExact(all.o) ? PyDict_GetItemWithError(all.o, key.o) : nullptr;
+        const at::Tensor *const t = o ? tensor(o, 1, at::kByte) : nullptr;
+        if (!t || t->size(0) < need) return nullptr;
+        Py_INCREF(o);
+        room.o = o;
+        return t;
+    }
+    bool take() { return taken = PyDict_DelItem(all.o, key.o) == 0; }
+    ~Kept() {
+        if (!taken) return;
+        PyObject *type, *value, *trace;   // an error that is on its way stays
+        PyErr_Fetch(&type, &value, &trace);
+        if (PyDict_SetItem(all.o, key.o, room.o)) PyErr_Clear();
+        PyErr_Restore(type, value, trace);
+    }
+};
+
 // attend(cache, q, table, lengths, scale or None, window, out or None, lse or None, workspace or None, stream or None) -> (out, lse).  Without a workspace the
 // one that the cache keeps for the stream is used, if there is one and it is large enough.
 PyObject *attend(PyObject *const *a, Py_ssize_t n) {
@@ -232,21 +259,15 @@ PyObject *attend(PyObject *const *a, Py_ssize_t n) {
     const int width = (int)tt->size(1);
     if (tq->size(2) != cache->head_dim || ((a[6] == Py_None || a[7] == Py_None) && a[9] != Py_None) || !stream_of(a[9], &stream)) return nullptr;
     if (p_room(cache, q.heads, requests, width, &need) != AMAP_OK) return nullptr;
-    Ref kept;
-    PyObject *room = a[8];
-    if (need && room == Py_None) {
-        if (a[9] != Py_None) return nullptr;
-        Ref all(PyObject_GetAttr(a[0], s_work)), key(PyLong_FromVoidPtr(stream));
-        if (!all.o || !key.o || !PyDict_CheckExact(all.o)) return nullptr;
-        room = PyDict_GetItemWithError(all.o, key.o);
-        if (!room) return nullptr;
-        kept.o = again(room);
-        Ref capturing(PyObject_CallNoArgs(is_capturing));   // (a graph runs beside what its stream does later: it has one of its own)
-        if (!capturing.o || PyObject_IsTrue(capturing.o)) return nullptr;
-    }
+    Kept kept;
     if (need) {
-        const at::Tensor *const tw = tensor(room, 1, at::kByte);
+        if (a[8] == Py_None && a[9] != Py_None) return nullptr;
+        const at::Tensor *const tw = a[8] == Py_None ? kept.look(a[0], stream, need) : tensor(a[8], 1, at::kByte);
         if (!tw || tw->size(0) < need) return nullptr;
+        if (a[8] == Py_None) {
+            Ref capturing(PyObject_CallNoArgs(is_capturing));   // (a graph runs beside what its stream does later: it has one of its own)
+            if (!capturing.o || PyObject_IsTrue(capturing.o) || !kept.take()) return nullptr;
+        }
         work = data<void>(*tw);
         have = tw->size(0);
     }

@@ -188,7 +188,9 @@ class PagedCache:
         self._c = B.amap_cache(k.data_ptr(), v.data_ptr(), _ELEMENT[k.dtype], k.size(0), k.size(1), k.size(2), k.size(3), k.stride(0), k.stride(1), k.stride(2),
                                None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
         self._cache_at = B.C.addressof(self._c)
-        self._work = {}   # cache_attend's workspace on each stream that it has been called on: one call after the other uses it there
+        # cache_attend's workspace on each stream that it has been called on: one call after the other uses it there.  A call takes it out while it issues its
+        # launches, so that no call of another thread finds it before they are all on the stream.
+        self._work = {}
 
     # (the library has their addresses)
     k, v, k_scale, v_scale = (property(operator.attrgetter(name)) for name in ("_k", "_v", "_k_scale", "_v_scale"))
@@ -326,7 +328,8 @@ def cache_append(cache, k, v, slot, rope=None, position=None, q=None, q_out=None
 def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=None, workspace=None, stream=None):
     """(out, lse): the attention of q [requests, heads, head_dim] over the first length[r] tokens (int32; window > 0: the last
     `window` of them) that table [requests, width] (int32) leads to.  scale: 1 / sqrt(head_dim) if None.  A request that sees nothing has
-    rows of 0 and lse -inf.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it."""
+    rows of 0 and lse -inf.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it; calls that may run at the same time, or
+    that two threads issue on one stream at the same time, must not be given the same one."""
     what = "amap_cache_attend"
     done = _native_attend(cache, q, table, length, scale, window, out, lse, workspace, stream)
     if done is not None:
@@ -336,7 +339,7 @@ def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=No
     _on_gpu(table, torch.int32, 2, what, "table")
     if _on_gpu(length, torch.int32, 1, what, "length").size(0) != n or table.size(0) != n or dim != cache.k.size(3):
         raise _refused(what, "q, table, length and the cache differ in requests or head_dim", B.AMAP_E_SHAPE)
-    need = attend_workspace(cache, heads, n, table.size(1))
+    need, keep = attend_workspace(cache, heads, n, table.size(1)), False
     with _made_on(stream):
         if out is None:
             out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
@@ -344,8 +347,7 @@ def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=No
             lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
         if workspace is None and need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-            if stream is None and not _capturing():   # (a graph's memory is the graph's)
-                cache._work[current_stream()] = workspace
+            keep = stream is None and not _capturing()   # (a graph's memory is the graph's)
     if isinstance(out, torch.Tensor) and out.shape != q.shape:
         raise _refused(what, f"out is {tuple(out.shape)}, not {tuple(q.shape)}", B.AMAP_E_SHAPE)
     if _on_gpu(lse, torch.float32, 2, what, "lse").shape != (n, heads) or not lse.is_contiguous():
@@ -354,6 +356,8 @@ def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=No
     B.amap_cache_attend(cache._c, a, n, table.data_ptr(), table.stride(0), table.size(1), length.data_ptr(), dim ** -0.5 if scale is None else scale, window,
                         _rows(out, what, "out"), lse.data_ptr(), None if workspace is None else workspace.data_ptr(), have,
                         current_stream() if stream is None else stream)
+    if keep:   # (from here on: its launches are on the stream)
+        cache._work[current_stream()] = workspace
     return out, lse
 
 
