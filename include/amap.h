@@ -507,7 +507,7 @@ amap_status amap_cache_append(const amap_cache *cache, const amap_heads *k, cons
 /* Attention of one new token per request over its cache: s_i = scale q . k_i over the tokens i < length[r] (window > 0: the last
  * `window` of them) whose page lies in the cache, out = sum softmax(s)_i v_i, lse (may be NULL) = log sum exp s_i, [requests, heads] row
  * by row.  A row that sees no token, or whose scores are all -inf, is 0 with lse -inf.  Heads heads / kv_heads * h .. share key head h.  What lies in
- * the cache outside the visible tokens is never used, whatever it holds.  A length beyond the table's width counts as
+ * the cache outside the visible tokens is never used, whatever it holds; a visible value that is infinite or NaN counts as the formula has it, however small its weight.  A length beyond the table's width counts as
  * that.  q and out: BF16 or F16 alike; head_dim a multiple of 8 (E4M3: 16) up to 256, rows of the cache 16-byte aligned.
  * workspace: amap_cache_attend_workspace bytes, 16-byte aligned; its contents need not be kept.  A call issues up to two launches, and the second reads
  * what the first left there: two calls may have the same workspace only if all launches of one are on the stream before the other is called. */

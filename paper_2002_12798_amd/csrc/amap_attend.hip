@@ -15,7 +15,10 @@
 //     V^T P^T, takes from it, so weights never leave their lane.  V comes transposed out of LDS (ds_read_tr).
 //   A weight is kept in two 16-bit parts, itself rounded and what that leaves: one part alone would be off by as much as
 //     the result's own rounding is.  With up to 8 queries to a key head the second part costs nothing: it takes the columns that are
-//     idle.  (A value that is infinite makes its column NaN, as 0 * inf does in the sum itself where a weight has vanished.)
+//     idle.
+//   An infinite value times a second part of 0 or of the other sign, or times a weight that has vanished in 32 bits, is NaN where the sum itself is infinite.  So a
+//     result that is not finite is looked at again: the same tiles with one weight, positive in both parts, for every score but -inf, and what is not finite then (infinite,
+//     or NaN of NaN, of both signs, or of an infinite score) takes the place of what was stored.  Whoever has no infinite values pays for the look: a multiply-add to a result.
 // Measured, cold: two requests of 131072 tokens, 32 queries to 8 key heads of 128, bf16 (1.07 GB) 181 us, 5.9 TB/s; 64 ragged ones up to 4096 (140 MB) 33.5 us, 28 of
 // them over shares and 5 of joining; 128 up to 2048 of an 8-bit cache, 12 heads of 64 (54 MB) 19 us; one of 500, 16 heads of 64, 6.5 us.
 #include "amap_cache.hpp"
@@ -81,6 +84,7 @@ struct Of<Bf16> {
     typedef __bf16 one;
     typedef bf16x8 eight;
     static constexpr float UP = 0.f;   // weights are kept times 2^UP
+    static constexpr float ALIKE = 0x1p-30f * (1.f + 0x1p-10f);   // the one weight of a second look: both parts positive, 2^31 of the largest values no overflow
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t x, bool high) {
         return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true))
@@ -94,6 +98,7 @@ struct Of<F16> {
     // 2^15 times a weight (at most 1) is the largest that fits; without it all of a long cache's weights under 2^-25 would vanish beside one key of weight 1,
     // 131072 of them at 2^-26 0.2 % of the sum
     static constexpr float UP = 15.f;
+    static constexpr float ALIKE = 1.f + 0x1p-12f;
     static __device__ __forceinline__ f32x4 product(eight a, eight b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ uint32_t two_of_e4m3(uint32_t x, bool high) {
         return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true))
@@ -112,6 +117,7 @@ struct Form {
     typedef T_ T;
     static constexpr int ES = ES_, DP = DP_;
     static constexpr bool PAIRED = PAIRED_;                 // the weights' second parts in columns 8 .. 15
+    static constexpr bool INFINITE = ES_ == 2;              // whether a value can be infinite
     static constexpr int ROW = DP * ES, NC = ROW / 16;      // bytes and 16-byte pieces of a row in LDS
     static constexpr int STAGES = 2;
     static constexpr int SIDE = kTokens * ROW, STAGE = 2 * SIDE;
@@ -277,8 +283,8 @@ __device__ __forceinline__ Lane<F> lane_of(const AttendArgs &a, uint32_t lane, u
 }
 
 // `steps` tiles of a segment from token `begin` on by one wavefront: the results of all its columns, not yet divided (o), a column's largest score less UP
-// (m, in powers of two) and this lane's part of the column's sum of weights (l).
-template <class F>
+// (m, in powers of two) and this lane's part of the column's sum of weights (l).  AGAIN, the second look: with the weight ALIKE for all scores but -inf, m of no use.
+template <class F, bool AGAIN>
 __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Lane<F> &w, uint32_t r, uint32_t kv, uint32_t head0, uint32_t rows, const Seen &seen, uint32_t begin,
                                              uint32_t steps, f32x4 (&o)[F::DP / 16], float &m, float &l) {
     typedef typename Of<typename F::T>::eight eight;
@@ -316,7 +322,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Lane<F> 
         shown[slot] = (uint32_t)__ballot(there);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the keys that were here have been read, and the pages
         if constexpr (2 * LV + LK + LK > 63) landed<63 - LK>();   // no more than the counter holds
-        fast = F::HALVES && a.halves && shown[slot] == 0xFFFFFFFFu;
+        fast = !AGAIN && F::HALVES && a.halves && shown[slot] == 0xFFFFFFFFu;   // (a second look is rare: the one form of loads that takes all)
         if (fast) {
             const uint32_t j0 = fdiv(t0, a.by_page), j1 = fdiv(t0 + 16u, a.by_page), id0 = __builtin_amdgcn_readlane(id, 0), id1 = __builtin_amdgcn_readlane(id, 16);
             const uint32_t x0 = id0 * a.page_step + (t0 - j0 * a.page) * a.token_step + kv * a.head_step;
@@ -366,7 +372,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Lane<F> 
     asm volatile("" ::"v"(by));
 #pragma unroll
     for (int i = 0; i < F::DP / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m = -INFINITY;
+    m = AGAIN ? INFINITY : -INFINITY;   // (INFINITY: never another, nothing is scaled)
     l = 0.f;
     landed<0>();   // the first pages, and the queries
     load_keys(0, 0);
@@ -417,7 +423,12 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Lane<F> 
         }
         float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(x[j] - from);
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (AGAIN)
+                p[j] = x[j] == -INFINITY ? 0.f : Of<typename F::T>::ALIKE + (x[j] - x[j]);   // (NaN for a score of inf or NaN)
+            else
+                p[j] = __builtin_amdgcn_exp2f(x[j] - from);
+        }
         l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         eight pf, rest;
 #pragma unroll
@@ -461,6 +472,25 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Lane<F> 
         step(s, std::integral_constant<int, 0>{});
         if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>{});
     }
+}
+
+// whether one of a wavefront's results is not finite
+template <class F>
+__device__ __forceinline__ bool any_infinite(const f32x4 (&o)[F::DP / 16]) {
+    if constexpr (!F::INFINITE) return false;
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < F::DP / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_fmaf(o[i][e], 0.f, x);
+    return __any(x != x);
+}
+
+// The kernel's arguments once more, for the second look: read there, not kept in scalar registers all the way.  (They are its only ones: offset 0.)
+__device__ __forceinline__ const AttendArgs &arguments_again() {
+    auto p = (const __attribute__((address_space(4))) AttendArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const AttendArgs *)p;
 }
 
 template <class F>
@@ -541,38 +571,52 @@ __global__ __launch_bounds__(64, (F::PER_UNIT + 3) / 4) void amap_attend_kernel(
         const uint32_t q0 = block * a.columns, rows = min(a.group - q0, a.columns);   // queries of the block
         const uint32_t head0 = kv * a.group + q0;
 
-        f32x4 o[F::DP / 16];
-        float m, l;
-        attend_tiles<F>(a, w, r, kv, head0, rows, seen, (seen.tile + tile) * kTokens, n, o, m, l);
+        const bool whole = tile == 0 && n == seen.tiles;
+        bool look = false;
+        const auto attend_piece = [&](const AttendArgs &a, auto second) __attribute__((always_inline)) {
+            constexpr bool AGAIN = decltype(second)::value;
+            f32x4 o[F::DP / 16];
+            float m, l;
+            attend_tiles<F, AGAIN>(a, w, r, kv, head0, rows, seen, (seen.tile + tile) * kTokens, n, o, m, l);
+            if constexpr (!AGAIN) look = any_infinite<F>(o);
 
-        // ---- the results, through LDS (in the place of the stages) into rows; a piece of a segment into the workspace
-        l = sum_of_column(l);
-        const bool whole = tile == 0 && n == seen.tiles, none = l == 0.f;   // (none: scores of -inf only)
-        float *const part = a.parts + (size_t)(2u * blockIdx.x + (tile == 0)) * kPart;   // the first piece of a segment, or a later one
-        const float vs = whole ? (none ? 0.f : (a.v_scale ? a.v_scale[kv] : 1.f) / l) : 1.f;
-        if (lane < rows) {
-            if (!whole)
-                part[lane] = m, part[kColumns + lane] = l;
-            else if (a.lse)
-                a.lse[(int64_t)r * a.heads + head0 + lane] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-        }
-#pragma unroll
-        for (int i = 0; i < F::DP / 16; ++i) lds_put<f32x4>(base + 4u * (col * F::OUT_ROW + 16u * i + 4u * g), none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[i] * vs);
-        for (uint32_t i = lane; i < rows * (F::DP / 4); i += 64u) {
-            const uint32_t c = i / (F::DP / 4), d = 4u * (i % (F::DP / 4)), at = base + 4u * (c * F::OUT_ROW + d);
-            f32x4 x = lds_at<f32x4>(at);
-            if constexpr (F::PAIRED) x += lds_at<f32x4>(at + 4u * 8u * F::OUT_ROW);
-            if (!whole) {
-                *reinterpret_cast<f32x4 *>(part + 2 * kColumns + 4 * i) = x;
-            } else {
-                typename Of<typename F::T>::one *const out =
-                    reinterpret_cast<typename Of<typename F::T>::one *>(a.out) + (int64_t)r * a.out_token + (int64_t)(head0 + c) * a.out_head + d;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (d + e < a.dim) out[e] = (typename Of<typename F::T>::one)x[e];
+            // ---- the results, through LDS (in the place of the stages) into rows; a piece of a segment into the workspace
+            l = sum_of_column(l);
+            const bool none = l == 0.f;   // (scores of -inf only)
+            float *const part = a.parts + (size_t)(2u * blockIdx.x + (tile == 0)) * kPart;   // the first piece of a segment, or a later one
+            const float vs = whole ? (none ? 0.f : (a.v_scale ? a.v_scale[kv] : 1.f) / l) : 1.f;
+            if (!AGAIN && lane < rows) {
+                if (!whole)
+                    part[lane] = m, part[kColumns + lane] = l;
+                else if (a.lse)
+                    a.lse[(int64_t)r * a.heads + head0 + lane] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
             }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, before the next segment's loads land there
+#pragma unroll
+            for (int i = 0; i < F::DP / 16; ++i) lds_put<f32x4>(base + 4u * (col * F::OUT_ROW + 16u * i + 4u * g), none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[i] * vs);
+            for (uint32_t i = lane; i < rows * (F::DP / 4); i += 64u) {
+                const uint32_t c = i / (F::DP / 4), d = 4u * (i % (F::DP / 4)), at = base + 4u * (c * F::OUT_ROW + d);
+                f32x4 x = lds_at<f32x4>(at);
+                if constexpr (F::PAIRED) x += lds_at<f32x4>(at + 4u * 8u * F::OUT_ROW);
+                if (!whole) {
+                    if constexpr (!AGAIN)
+                        *reinterpret_cast<f32x4 *>(part + 2 * kColumns + 4 * i) = x;
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!__builtin_isfinite(x[e])) part[2 * kColumns + 4 * i + e] = x[e];
+                } else {
+                    typename Of<typename F::T>::one *const out =
+                        reinterpret_cast<typename Of<typename F::T>::one *>(a.out) + (int64_t)r * a.out_token + (int64_t)(head0 + c) * a.out_head + d;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (d + e < a.dim && (!AGAIN || !__builtin_isfinite(x[e]))) out[e] = (typename Of<typename F::T>::one)x[e];
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, before the next loads land there
+        };
+        attend_piece(a, std::false_type{});
+        if constexpr (F::INFINITE)
+            if (__builtin_expect(look, 0)) attend_piece(arguments_again(), std::true_type{});
         if (a.splits && tile == 0 && lane == 0) a.splits[r * a.segments + segment] = Split{blockIdx.x, whole ? 0u : (u - at + seen.units - 1) / share - blockIdx.x + 1};
         u += past - at;
         at = 0;
@@ -649,6 +693,19 @@ __global__ __launch_bounds__(THREADS) void amap_attend_join_kernel(const JoinArg
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (d + e < a.dim) out[d + e] = (typename Of<T>::one)(none ? 0.f : x[e] * by);
+            // (a factor may be 0: what is infinite or NaN in a piece is that in the result)
+            if (__builtin_expect(!__builtin_isfinite((x[0] + x[1]) + (x[2] + x[3])), 0)) {
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (uint32_t p = 0; p < s.count; ++p) {
+                    const f32x4 z = *reinterpret_cast<const f32x4 *>(first + (size_t)(p ? 2u * p : 1u) * kPart + 2 * kColumns + c * DP + d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] += __builtin_isfinite(z[e]) ? 0.f : z[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (d + e < a.dim && !__builtin_isfinite(y[e])) out[d + e] = (typename Of<T>::one)(none ? 0.f : y[e] * by);
+            }
             if (lane == 0 && a.lse) a.lse[(int64_t)r * a.heads + h] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
         }
         __syncthreads();
@@ -668,44 +725,57 @@ __global__ __launch_bounds__(64 * F::PER_UNIT, (F::PER_UNIT + 3) / 4) void amap_
     const Seen seen = seen_of(a, a.length[r]);
     const uint32_t each = (seen.tiles + waves - 1) / waves, first = wave * each, n = first < seen.tiles ? min(each, seen.tiles - first) : 0u;
     const uint32_t base = stages + wave * F::LDS, stats = F::STAGES * F::STAGE;   // stats: of a wavefront's LDS, maxima and sums of its columns
-    if (n) {
-        const Lane<F> w = lane_of<F>(a, lane, base);
-        f32x4 o[F::DP / 16];
-        float m, l;
-        attend_tiles<F>(a, w, r, kv, head0, rows, seen, (seen.tile + first) * kTokens, n, o, m, l);
-        l = sum_of_column(l);
-#pragma unroll
-        for (int i = 0; i < F::DP / 16; ++i) lds_put<f32x4>(base + 4u * (w.col * F::OUT_ROW + 16u * i + 4u * w.g), o[i]);
-        if (lane < kColumns) {
-            lds_put<float>(base + stats + 4u * lane, m);
-            lds_put<float>(base + stats + 64u + 4u * lane, l);
-        }
-    }
-    __syncthreads();
-    const uint32_t parts = each ? (seen.tiles + each - 1) / each : 0u;   // wavefronts that had something
+    const uint32_t parts = each ? (seen.tiles + each - 1) / each : 0u;   // wavefronts that have something
     const float vs = a.v_scale ? a.v_scale[kv] : 1.f;
-    for (uint32_t i = threadIdx.x; i < rows * (F::DP / 4); i += blockDim.x) {
-        const uint32_t c = i / (F::DP / 4), d = 4u * (i % (F::DP / 4));
-        float high = -INFINITY, sum = 0.f;
-        for (uint32_t p = 0; p < parts; ++p) high = fmaxf(high, lds_at<float>(stages + p * F::LDS + stats + 4u * c));
-        const float from = high == -INFINITY ? 0.f : high;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t p = 0; p < parts; ++p) {
-            const uint32_t at = stages + p * F::LDS;
-            const float take = __builtin_amdgcn_exp2f(lds_at<float>(at + stats + 4u * c) - from);
-            sum += take * lds_at<float>(at + stats + 64u + 4u * c);
-            f32x4 y = lds_at<f32x4>(at + 4u * (c * F::OUT_ROW + d));
-            if constexpr (F::PAIRED) y += lds_at<f32x4>(at + 4u * ((c + 8u) * F::OUT_ROW + d));
-            x += y * take;
-        }
-        const bool none = sum == 0.f;   // (nothing seen, or scores of -inf only)
-        const float by = none ? 0.f : vs / sum;
-        one *const out = reinterpret_cast<one *>(a.out) + (int64_t)r * a.out_token + (int64_t)(head0 + c) * a.out_head + d;
+    uint32_t look = 0;
+    const auto attend_segment = [&](const AttendArgs &a, auto second) __attribute__((always_inline)) {
+        constexpr bool AGAIN = decltype(second)::value;
+        if (n) {
+            const Lane<F> w = lane_of<F>(a, lane, base);
+            f32x4 o[F::DP / 16];
+            float m, l;
+            attend_tiles<F, AGAIN>(a, w, r, kv, head0, rows, seen, (seen.tile + first) * kTokens, n, o, m, l);
+            l = sum_of_column(l);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (d + e < a.dim) out[e] = (one)(none ? 0.f : x[e] * by);
-        if (d == 0 && a.lse) a.lse[(int64_t)r * a.heads + head0 + c] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
-    }
+            for (int i = 0; i < F::DP / 16; ++i) lds_put<f32x4>(base + 4u * (w.col * F::OUT_ROW + 16u * i + 4u * w.g), o[i]);
+            if (lane < kColumns) {
+                lds_put<float>(base + stats + 4u * lane, AGAIN ? 0.f : m);
+                lds_put<float>(base + stats + 64u + 4u * lane, l);
+            }
+            if constexpr (F::INFINITE && !AGAIN) lds_put<uint32_t>(base + stats + 128u, any_infinite<F>(o));
+        }
+        __syncthreads();
+        if constexpr (F::INFINITE && !AGAIN)
+            for (uint32_t p = 0; p < parts; ++p) look |= lds_at<uint32_t>(stages + p * F::LDS + stats + 128u);
+        for (uint32_t i = threadIdx.x; i < rows * (F::DP / 4); i += blockDim.x) {
+            const uint32_t c = i / (F::DP / 4), d = 4u * (i % (F::DP / 4));
+            float high = -INFINITY, sum = 0.f;
+            for (uint32_t p = 0; p < parts; ++p) high = fmaxf(high, lds_at<float>(stages + p * F::LDS + stats + 4u * c));
+            const float from = high == -INFINITY ? 0.f : high;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            for (uint32_t p = 0; p < parts; ++p) {
+                const uint32_t at = stages + p * F::LDS;
+                const float take = __builtin_amdgcn_exp2f(lds_at<float>(at + stats + 4u * c) - from);
+                sum += take * lds_at<float>(at + stats + 64u + 4u * c);
+                f32x4 y = lds_at<f32x4>(at + 4u * (c * F::OUT_ROW + d));
+                if constexpr (F::PAIRED) y += lds_at<f32x4>(at + 4u * ((c + 8u) * F::OUT_ROW + d));
+                x += y * take;
+            }
+            const bool none = sum == 0.f;   // (nothing seen, or scores of -inf only)
+            const float by = none ? 0.f : vs / sum;
+            one *const out = reinterpret_cast<one *>(a.out) + (int64_t)r * a.out_token + (int64_t)(head0 + c) * a.out_head + d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (d + e < a.dim && (!AGAIN || !__builtin_isfinite(x[e]))) out[e] = (one)(none ? 0.f : x[e] * by);
+            if (!AGAIN && d == 0 && a.lse) a.lse[(int64_t)r * a.heads + head0 + c] = none ? -INFINITY : (high + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+    };
+    attend_segment(a, std::false_type{});
+    if constexpr (F::INFINITE)
+        if (__builtin_expect(look != 0u, 0)) {
+            __syncthreads();   // (the results have been read: the stages are in their place)
+            attend_segment(arguments_again(), std::true_type{});
+        }
 }
 
 // How a call is cut: workgroups, columns of a block, and whether a segment may be split between workgroups.

@@ -1,0 +1,74 @@
+"""What the operators around the paged cache give at values that an ordinary test does not meet: infinities among the visible values.  Needs an MI355X (-m gpu)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_cache import BF16, F16, HALF_STEP, SMALLEST, _close, _expect, _f64, _requests
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    from paper_2002_12798_amd import device
+    device.require_gpu()
+    return device
+
+
+# ---- infinite values
+
+def _check_with_infinities(got, want, q, keys):
+    """Elements that are not finite are the same ones; the others within what test_gpu_cache allows them."""
+    out, lse, mass, most = want
+    g, finite = _f64(got[0]), np.isfinite(out)
+    assert np.array_equal(g[~finite], out[~finite], equal_nan=True)
+    score = (q.shape[2] + 4) * 2.0 ** -24 * most
+    weight = np.broadcast_to((2 * score + 2.0 ** -21 + 2.0 ** -16 + 2 * keys * 2.0 ** -24)[:, :, None], out.shape)
+    off = 2 * weight[finite] * mass[finite]
+    _close(g[finite], out[finite], HALF_STEP[q.dtype] * (np.abs(out[finite]) + off) + off + SMALLEST[q.dtype])
+    none = lse == -np.inf
+    _close(_f64(got[1])[~none], lse[~none], (score + 2.0 ** -21 + keys * 2.0 ** -24 + 2.0 ** -22 * np.abs(np.where(none, 0, lse)))[~none])
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("heads, kv, dim, dtype", [(4, 4, 64, BF16), (8, 1, 128, F16), (16, 1, 64, BF16), (16, 1, 96, F16), (20, 1, 128, F16), (24, 2, 256, BF16), (12, 1, 80, F16)])
+def test_infinite_values(dev, heads, kv, dim, dtype, wide):
+    """The definition's: infinite where one of a sign is seen, however small its weight, NaN where both signs are; other elements and rows as ever.
+    In a request of one token, of one tile, and of several shares."""
+    lengths = [1, 20, 300, 2500]
+    cache, q, table, length = _requests(dev, dim + heads, lengths, heads, kv, dim, 16, dtype, dtype, "tokens")
+    v = cache.v
+    place = lambda r, i: (table[r, i // 16].item(), i % 16)  # noqa: E731
+    for r, n in enumerate(lengths):
+        for i, d, x in ((0, 1, math.inf), (n - 1, 3, -math.inf), (n // 2, 4, math.inf), (n // 3, 4, -math.inf), (n - 1, 6, math.nan), (n // 2, dim - 1, math.inf)):
+            v[(*place(r, i), slice(None), d)] = x
+    # tokens whose weights are 2^-30 to 2^-100 of the largest
+    q.abs_().add_(0.01)
+    for r, i, below in ((2, 100, 30), (2, 101, 45), (3, 40, 60), (3, 2400, 100)):
+        at = place(r, i)
+        for h in range(kv):
+            mean = _f64(q)[r, h * (heads // kv)].sum() * dim ** -0.5
+            cache.k[(*at, h)] = -below * math.log(2) / mean
+        v[(*at, slice(None), 8 + i % 7)] = math.inf
+    if wide:
+        table = torch.cat([table, torch.full((len(lengths), 3000), -1, dtype=torch.int32)], 1)
+    got = dev.cache_attend(cache, q, table.cuda(), length.cuda())
+    want = _expect(cache, q, table, length, dim ** -0.5)
+    assert np.isposinf(want[0][:, :, 1]).all() and np.isnan(want[0][1:, :, 4]).all() and np.isfinite(want[0][:, :, 20]).all()
+    _check_with_infinities(got, want, q, max(lengths))
+
+
+def test_values_that_became_infinite_in_the_store(dev):
+    """32-bit values beyond fp16's largest are infinite in the cache, and in what is read from it."""
+    k, v = (torch.zeros((2, 16, 1, 64), dtype=F16, device="cuda") for _ in range(2))
+    cache = dev.PagedCache(k, v)
+    new = torch.zeros((3, 1, 64), device="cuda")
+    new[1, 0, 5], new[2, 0, 7] = 1e6, -7e4
+    dev.cache_append(cache, torch.zeros_like(new), new, torch.arange(3, device="cuda"))
+    q = torch.ones((1, 2, 64), dtype=F16, device="cuda")
+    out, lse = dev.cache_attend(cache, q, torch.tensor([[0]], dtype=torch.int32, device="cuda"), torch.tensor([3], dtype=torch.int32, device="cuda"))
+    want = torch.zeros((1, 2, 64), device="cuda")
+    want[..., 5], want[..., 7] = math.inf, -math.inf
+    assert torch.equal(out.float(), want)
