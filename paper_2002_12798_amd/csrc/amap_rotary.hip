@@ -536,8 +536,11 @@ extern "C" amap_status amap_cache_append(const amap_cache *cache, const amap_hea
         st = check_turn(q, q_out, tokens, dim, rows[2], to);
         if (st != AMAP_OK) return st;
         if (meet(to, ck) || meet(to, cv)) return AMAP_E_ALIAS;
-        // (q may lie between k and v in one projection, and be turned there in place)
-        if (!same_rows(*q, *q_out) && (meet(to, rows[0]) || meet(to, rows[1]))) return AMAP_E_ALIAS;
+        // (q may lie beside k and v in one projection, and be turned there in place)
+        for (int i = 0; i < 2; ++i) {
+            const bool met = same_rows(*q, *q_out) ? share(*q_out, i ? *v : *k, tokens, dim) : meet(to, rows[i]);
+            if (met) return AMAP_E_ALIAS;
+        }
         way[n++] = Way{q, q_out->data, q_out->type, q_out->token_stride, q_out->head_stride, 0, true, false, nullptr};
     }
     for (int i = 0; i < n; ++i)

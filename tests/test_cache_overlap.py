@@ -1,0 +1,63 @@
+"""Tensors of a call around the paged cache that have elements in common, where one is written: refused.  Tensors that only lie between one another's rows: taken."""
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2002_12798_amd import binding as B
+from tests.test_cache_args import AT, _cache, _refuses, _rope, _rows
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_whether_tensors_share_an_element(tmp_path):
+    """The host's answer against every byte, built with the host's compiler."""
+    exe = str(tmp_path / "overlap_check")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=undefined", "-I", os.path.join(ROOT, "include"),
+                           "-I", os.path.join(ROOT, "paper_2002_12798_amd", "csrc"), os.path.join(ROOT, "tests", "overlap_check.cpp"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
+# [10 tokens, 8 heads, 64] of 2 bytes: q, k and v are heads of it
+HEAD, TOKEN = 128, 512
+
+
+@pytest.mark.parametrize("q, heads, k, v", [
+    (0, 2, 0, 6),      # q is k
+    (0, 3, 2, 6),      # one head of q is k's first
+    (3, 2, 2, 6),      # and k's last
+    (2, 4, 0, 4),      # the same for v
+    (0, 8, 0, 6),      # all of them
+])
+def test_queries_turned_in_place_over_keys_or_values(q, heads, k, v):
+    at = lambda h, n: _rows(6 * AT + HEAD * h, heads=n, token=TOKEN)  # noqa: E731
+    _refuses(B.AMAP_E_ALIAS, B.amap_cache_append, _cache(), at(k, 2), at(v, 2), 10, 7 * AT, _rope(), 7 * AT, 0, at(q, heads), at(q, heads))
+
+
+@pytest.mark.parametrize("more", [dict(token=500), dict(token=TOKEN, head=68), dict(token=TOKEN)])
+def test_queries_turned_in_place_between_other_strides(more):
+    """Strides that differ from the keys' are not looked into, and a projection whose rows begin half a head off has elements in common."""
+    off = 64 if more == dict(token=TOKEN) else 0
+    q = _rows(6 * AT + off, heads=2, **more)
+    _refuses(B.AMAP_E_ALIAS, B.amap_cache_append, _cache(), _rows(6 * AT + HEAD, token=TOKEN), _rows(5 * AT), 10, 7 * AT, _rope(), 7 * AT, 0, q, q)
+
+
+@pytest.mark.gpu
+def test_queries_turned_in_place_beside_keys_and_values():
+    """What is beside k and v, in front of them, between them or behind them, is taken and gives what a call into a tensor of its own gives."""
+    from paper_2002_12798_amd import device
+    g = torch.Generator().manual_seed(4)
+    packed = torch.randn((33, 9, 64), generator=g).bfloat16().cuda()
+    rope, position = device.Rope(torch.rand(32, generator=g).cuda()), torch.arange(33, dtype=torch.int32, device="cuda")
+    slot = torch.randperm(48, generator=g)[:33].cuda()
+    for q, heads, k, v in ((0, 5, 5, 7), (2, 5, 0, 7), (4, 5, 0, 2), (8, 1, 5, 2)):
+        caches = [[torch.zeros((3, 16, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2)]
+        want = device.cache_append(device.PagedCache(*caches[0]), packed[:, k:k + 2], packed[:, v:v + 2], slot, rope, position, packed[:, q:q + heads])
+        x = packed.clone()
+        part = x[:, q:q + heads]
+        assert device.cache_append(device.PagedCache(*caches[1]), x[:, k:k + 2], x[:, v:v + 2], slot, rope, position, part, part) is part
+        assert torch.equal(part, want) and torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
+        part.copy_(packed[:, q:q + heads])
+        assert torch.equal(x, packed)
