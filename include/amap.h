@@ -498,7 +498,8 @@ amap_status amap_rotary(const amap_heads *x, const amap_heads *out, int64_t toke
                         const int32_t *position, int64_t axis_stride, int inverse, void *stream);
 
 /* k and v of `tokens` tokens into the cache at their slots, rounded once to its type (E4M3: divided by the
- * head's scale, at most 448 either way).  Slots outside the cache are left out; no slot may come twice.  With a rope
+ * head's scale, at most 448 either way).  Slots outside the cache are left out; no slot may come twice, and the
+ * cache's keys and values share no element (amap_cache_attend, which only reads them, does not ask).  With a rope
  * (NULL: none) k is turned on the way, and q (NULL: none) into q_out as by amap_rotary, out of the cache's way and k's and v's: q may be
  * turned in place beside them in one projection (the same strides), but share no element with either. */
 amap_status amap_cache_append(const amap_cache *cache, const amap_heads *k, const amap_heads *v, int64_t tokens, const int64_t *slot,

@@ -94,4 +94,14 @@ inline bool share(const amap_heads &a, const amap_heads &b, int64_t tokens, int 
     return reach(s, 0, (int64_t)(reinterpret_cast<uintptr_t>(b.data) - reinterpret_cast<uintptr_t>(a.data)), es * dim);
 }
 
+// Whether a cache's keys and values, which have the same strides, have a byte in common.
+inline bool keys_and_values_share(const amap_cache &c) {
+    const int64_t es = bytes_of(c.type);
+    Steps s;
+    s.add(es * c.page_stride, 1 - c.n_pages, c.n_pages - 1);
+    s.add(es * c.token_stride, 1 - c.page_size, c.page_size - 1);
+    s.add(es * c.head_stride, 1 - c.kv_heads, c.kv_heads - 1);
+    return meet(box_of(c, c.k), box_of(c, c.v)) && reach(s, 0, (int64_t)(reinterpret_cast<uintptr_t>(c.v) - reinterpret_cast<uintptr_t>(c.k)), es * c.head_dim);
+}
+
 }  // namespace amap_cache_detail

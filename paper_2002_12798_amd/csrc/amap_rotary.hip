@@ -516,6 +516,7 @@ extern "C" amap_status amap_cache_append(const amap_cache *cache, const amap_hea
     Box ck, cv, rows[3], to;
     amap_status st = check_cache(cache, ck, cv);
     if (st != AMAP_OK) return st;
+    if (keys_and_values_share(*cache)) return AMAP_E_ALIAS;
     const int dim = cache->head_dim;
     if (!k || !v || (q != nullptr) != (q_out != nullptr) || (q && !rope)) return AMAP_E_INVALID;
     st = check_sizes(tokens, dim);

@@ -44,6 +44,32 @@ def test_queries_turned_in_place_between_other_strides(more):
     _refuses(B.AMAP_E_ALIAS, B.amap_cache_append, _cache(), _rows(6 * AT + HEAD, token=TOKEN), _rows(5 * AT), 10, 7 * AT, _rope(), 7 * AT, 0, q, q)
 
 
+# keys and values in one buffer; 8 pages of 16 tokens, 2 heads of 64, 2 bytes
+@pytest.mark.parametrize("over", [
+    dict(v=AT + 2 * 64),                                                          # the second head of the keys is the first of the values
+    dict(v=AT + 2 * 2048), dict(v=AT - 2 * 2048 * 7),                             # a page later; the keys' first page is the values' last
+    dict(v=AT + 2 * 128 * 15), dict(v=AT + 2), dict(k=2 * AT + 126),
+    dict(v=AT + 2 * 64, token_stride=256, page_stride=4096, head_stride=64),      # a token's heads beside one another, half of them in common
+    dict(v=AT + 2 * 2048, page_stride=64, token_stride=512, head_stride=8192),    # heads outermost
+])
+def test_keys_and_values_of_one_buffer_that_overlap(over):
+    _refuses(B.AMAP_E_ALIAS, B.amap_cache_append, _cache(**over), _rows(5 * AT), _rows(6 * AT), 10, 7 * AT)
+
+
+@pytest.mark.gpu
+def test_keys_and_values_of_one_buffer():
+    """A token's keys beside its values, head by head or all of them, and whole pages of either: no element in common."""
+    from paper_2002_12798_amd import device
+    x = torch.randn((20, 4, 64)).half().cuda()
+    slot = torch.randperm(48)[:20].cuda()
+    for shape, k, v in (((3, 16, 2, 2, 64), lambda t: t[:, :, :, 0], lambda t: t[:, :, :, 1]), ((3, 16, 4, 64), lambda t: t[:, :, :2], lambda t: t[:, :, 2:]),
+                        ((3, 2, 16, 2, 64), lambda t: t[:, 1], lambda t: t[:, 0]), ((6, 16, 2, 64), lambda t: t[3:], lambda t: t[:3])):
+        buffer = torch.zeros(shape, dtype=torch.float16, device="cuda")
+        device.cache_append(device.PagedCache(k(buffer), v(buffer)), x[:, :2], x[:, 2:], slot)
+        assert torch.equal(k(buffer)[slot // 16, slot % 16], x[:, :2]) and torch.equal(v(buffer)[slot // 16, slot % 16], x[:, 2:])
+        assert buffer.count_nonzero() == x.count_nonzero()
+
+
 @pytest.mark.gpu
 def test_queries_turned_in_place_beside_keys_and_values():
     """What is beside k and v, in front of them, between them or behind them, is taken and gives what a call into a tensor of its own gives."""
