@@ -492,7 +492,8 @@ typedef struct {
 amap_status amap_cache_assign(const amap_assign *a, void *stream);
 
 /* out = x with every pair turned (inverse: turned back, which is the gradient of the turn as well).  x and out have the
- * same type (F32, BF16, F16) and heads; out is x itself or does not overlap it.  Axis a of token t is at
+ * same type (F32, BF16, F16) and heads; out is x itself or shares no element with it: tensors that
+ * lie between one another's rows, as heads of one projection do, are told apart where their strides are the same.  Axis a of token t is at
  * position[a * axis_stride + t] (axis_stride 0: the same for all). */
 amap_status amap_rotary(const amap_heads *x, const amap_heads *out, int64_t tokens, int head_dim, const amap_rope *rope,
                         const int32_t *position, int64_t axis_stride, int inverse, void *stream);

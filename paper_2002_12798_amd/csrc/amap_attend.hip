@@ -927,7 +927,7 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     const int dim = cache->head_dim, es = bytes_of(cache->type);
     const Box from = box_of(*q, requests, dim), to = box_of(*out, requests, dim), k = box_of(*cache, cache->k), v = box_of(*cache, cache->v);
     if (!from.fits || !to.fits || !to.apart) return AMAP_E_SHAPE;
-    if (meet(to, from) || meet(to, k) || meet(to, v)) return AMAP_E_ALIAS;
+    if (share(*out, *q, requests, dim) || meet(to, k) || meet(to, v)) return AMAP_E_ALIAS;
     const uintptr_t q_at = reinterpret_cast<uintptr_t>(q->data);
     if ((q_at | reinterpret_cast<uintptr_t>(out->data)) % 2) return refuse("a tensor that does not begin at a whole element");
     Cut cut;

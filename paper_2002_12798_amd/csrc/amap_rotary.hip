@@ -479,13 +479,14 @@ amap_status check_rows(const amap_heads *h, int64_t tokens, int dim, bool writte
 
 bool same_rows(const amap_heads &a, const amap_heads &b) { return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride; }
 
+// (out is x itself, or beside it: in one projection, say)
 amap_status check_turn(const amap_heads *x, const amap_heads *out, int64_t tokens, int dim, Box &from, Box &to) {
     amap_status st = check_rows(x, tokens, dim, false, from);
     if (st == AMAP_OK) st = check_rows(out, tokens, dim, true, to);
     if (st != AMAP_OK) return st;
     if (x->type != out->type) return AMAP_E_INVALID;
     if (x->heads != out->heads) return AMAP_E_SHAPE;
-    return meet(from, to) && !same_rows(*x, *out) ? AMAP_E_ALIAS : AMAP_OK;
+    return !same_rows(*x, *out) && share(*x, *out, tokens, dim) ? AMAP_E_ALIAS : AMAP_OK;
 }
 
 amap_status check_sizes(int64_t tokens, int dim) {
@@ -538,10 +539,7 @@ extern "C" amap_status amap_cache_append(const amap_cache *cache, const amap_hea
         if (st != AMAP_OK) return st;
         if (meet(to, ck) || meet(to, cv)) return AMAP_E_ALIAS;
         // (q may lie beside k and v in one projection, and be turned there in place)
-        for (int i = 0; i < 2; ++i) {
-            const bool met = same_rows(*q, *q_out) ? share(*q_out, i ? *v : *k, tokens, dim) : meet(to, rows[i]);
-            if (met) return AMAP_E_ALIAS;
-        }
+        if (share(*q_out, *k, tokens, dim) || share(*q_out, *v, tokens, dim)) return AMAP_E_ALIAS;
         way[n++] = Way{q, q_out->data, q_out->type, q_out->token_stride, q_out->head_stride, 0, true, false, nullptr};
     }
     for (int i = 0; i < n; ++i)

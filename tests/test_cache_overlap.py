@@ -87,3 +87,32 @@ def test_queries_turned_in_place_beside_keys_and_values():
         assert torch.equal(part, want) and torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
         part.copy_(packed[:, q:q + heads])
         assert torch.equal(x, packed)
+
+
+@pytest.mark.gpu
+def test_outputs_beside_their_inputs():
+    """Heads of one projection turned into, or attended into, other heads of it; the rest of it stays.  Outputs that share a head or part of one are refused."""
+    from paper_2002_12798_amd import device
+    g = torch.Generator().manual_seed(5)
+    packed = torch.randn((21, 10, 64), generator=g).half().cuda()
+    rope, position = device.Rope(torch.rand(32, generator=g).cuda()), torch.arange(21, dtype=torch.int32, device="cuda")
+    k, v = (torch.randn((9, 16, 2, 64), generator=g).half().cuda() for _ in range(2))
+    cache, table = device.PagedCache(k, v), torch.randint(0, 9, (21, 4), generator=g, dtype=torch.int32).cuda()
+    length = torch.randint(0, 65, (21,), generator=g, dtype=torch.int32).cuda()
+    calls = (lambda x, out: device.rotary(x, rope, position, out=out), lambda x, out: device.cache_attend(cache, x, table, length, out=out)[0],
+             lambda x, out: device.cache_append(cache, packed[:, 8:], packed[:, 8:], torch.full((21,), -1, device="cuda"), rope, position, x, out))
+    for call in calls:
+        for of, to in ((0, 4), (4, 0), (2, 6), (0, 6)):
+            x = packed.clone()
+            want = call(x[:, of:of + 4].contiguous(), torch.empty((21, 4, 64), dtype=x.dtype, device="cuda"))
+            call(x[:, of:of + 4], x[:, to:to + 4])
+            assert torch.equal(x[:, to:to + 4], want)
+            x[:, to:to + 4] = packed[:, to:to + 4]
+            assert torch.equal(x, packed)
+        for of, to in ((0, 3), (3, 0), (1, 2)):
+            with pytest.raises(B.AmapError) as e:
+                call(packed[:, of:of + 4], packed[:, to:to + 4])
+            assert e.value.status == B.AMAP_E_ALIAS
+        with pytest.raises(B.AmapError) as e:
+            call(packed[:, :4, :], packed.view(-1)[4 * 64 - 2:].as_strided((21, 4, 64), packed.stride()))
+        assert e.value.status == B.AMAP_E_ALIAS
