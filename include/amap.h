@@ -48,7 +48,7 @@ typedef enum {
     AMAP_E_SHAPE = 2,        /* reshape volume mismatch, slice or pad out of range, concat extents */
     AMAP_E_UNSUPPORTED = 3,  /* e.g. reverse of a map that is not a bijection */
     AMAP_E_NOMEM = 4,
-    AMAP_E_ALIAS = 5,        /* dst overlaps a source */
+    AMAP_E_ALIAS = 5,        /* dst overlaps a source, or another array that the call writes */
     AMAP_E_HIP = 6           /* the HIP runtime reported an error at launch */
 } amap_status;
 
@@ -513,7 +513,7 @@ amap_status amap_cache_append(const amap_cache *cache, const amap_heads *k, cons
  * the cache outside the visible tokens is never used, whatever it holds; a visible value that is infinite or NaN counts as the formula has it, however small its weight.  A length beyond the table's width counts as
  * that.  q and out: BF16 or F16 alike; head_dim a multiple of 8 (E4M3: 16) up to 256, rows of the cache 16-byte aligned.
  * workspace: amap_cache_attend_workspace bytes, 16-byte aligned; its contents need not be kept.  A call issues up to two launches, and the second reads
- * what the first left there: two calls may have the same workspace only if all launches of one are on the stream before the other is called. */
+ * what the first left there (so out, lse and the workspace overlap neither one another nor anything that the call reads): two calls may have the same workspace only if all launches of one are on the stream before the other is called. */
 amap_status amap_cache_attend(const amap_cache *cache, const amap_heads *q, int64_t requests, const int32_t *table, int64_t table_stride,
                               int table_width, const int32_t *length, float scale, int window, const amap_heads *out, float *lse,
                               void *workspace, int64_t workspace_bytes, void *stream);

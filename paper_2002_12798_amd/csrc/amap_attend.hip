@@ -928,6 +928,9 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     const Box from = box_of(*q, requests, dim), to = box_of(*out, requests, dim), k = box_of(*cache, cache->k), v = box_of(*cache, cache->v);
     if (!from.fits || !to.fits || !to.apart) return AMAP_E_SHAPE;
     if (share(*out, *q, requests, dim) || meet(to, k) || meet(to, v)) return AMAP_E_ALIAS;
+    const int64_t rows_of_table[2] = {requests, table_width}, strides_of_table[2] = {table_stride, 1};
+    const Box entries = table_width ? box_of(table, 4, 2, rows_of_table, strides_of_table) : box_of(table, 0);
+    if (!entries.fits) return AMAP_E_SHAPE;
     const uintptr_t q_at = reinterpret_cast<uintptr_t>(q->data);
     if ((q_at | reinterpret_cast<uintptr_t>(out->data)) % 2) return refuse("a tensor that does not begin at a whole element");
     Cut cut;
@@ -935,6 +938,14 @@ extern "C" amap_status amap_cache_attend(const amap_cache *cache, const amap_hea
     if (st != AMAP_OK) return st;
     if (cut.bytes && (!workspace || workspace_bytes < cut.bytes)) return AMAP_E_INVALID;
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return refuse("a workspace that is not 16-byte aligned");
+    // what the call writes against one another and against all that it reads: lengths that changed on the way would give workgroups different shares, and pieces that were written over
+    // would name places outside the workspace
+    const Box sums = box_of(lse, lse ? 4 * requests * q->heads : 0), work = box_of(workspace, cut.bytes);
+    const Box read[] = {from, k, v, entries, box_of(length, 4 * requests), box_of(cache->k_scale, cache->k_scale ? 4 * cache->kv_heads : 0),
+                        box_of(cache->v_scale, cache->v_scale ? 4 * cache->kv_heads : 0)};
+    for (const Box &b : read)
+        if (meet(sums, b) || meet(work, b) || (&b != read && meet(to, b))) return AMAP_E_ALIAS;
+    if (meet(sums, to) || meet(work, to) || meet(sums, work)) return AMAP_E_ALIAS;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const StreamDevice device(s);
     if (device.status() != hipSuccess) return launched(device.status(), "the stream's device");

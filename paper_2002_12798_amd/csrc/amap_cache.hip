@@ -129,18 +129,12 @@ __global__ __launch_bounds__(kAssignThreads) void amap_assign_kernel(const Assig
 
 // Whether an array that the call writes meets another one of its arrays (outputs would be read as lengths by workgroups that come later).
 bool any_meet(const amap_assign &a) {
-    const auto of = [](const void *data, int64_t bytes) {
-        Box b;
-        b.first = reinterpret_cast<uintptr_t>(data);
-        b.past = b.first + (uintptr_t)bytes;
-        return b;
-    };
     const int64_t rows = a.requests && a.table_width ? (a.requests - 1) * a.table_stride + a.table_width : 0;
-    const Box all[] = {of(a.table, 4 * rows), of(a.begin, 4 * (a.requests + 1)), of(a.length, 4 * a.requests), of(a.slot, 8 * a.n_tokens), of(a.position, 4 * a.n_tokens),
-                       of(a.owner, 4 * a.n_tokens), of(a.taken, 4), of(a.cached, a.cached ? 4 * a.requests : 0), of(a.fresh, 4 * a.requests), of(a.free_pages, 4 * a.n_free)};
+    const Box all[] = {box_of(a.table, 4 * rows), box_of(a.begin, 4 * (a.requests + 1)), box_of(a.length, 4 * a.requests), box_of(a.slot, 8 * a.n_tokens), box_of(a.position, 4 * a.n_tokens),
+                       box_of(a.owner, 4 * a.n_tokens), box_of(a.taken, 4), box_of(a.cached, a.cached ? 4 * a.requests : 0), box_of(a.fresh, 4 * a.requests), box_of(a.free_pages, 4 * a.n_free)};
     for (int i = 0; i < 7; ++i)
         for (int j = i + 1; j < 10; ++j)
-            if (all[i].first < all[i].past && all[j].first < all[j].past && meet(all[i], all[j])) return true;
+            if (meet(all[i], all[j])) return true;
     return false;
 }
 

@@ -42,8 +42,16 @@ inline Box box_of(const void *data, int64_t es, int n, const int64_t *extent, co
     }
     return b;
 }
-inline bool meet(const Box &a, const Box &b) { return a.first < b.past && b.first < a.past; }
+inline bool meet(const Box &a, const Box &b) { return a.first < a.past && b.first < b.past && a.first < b.past && b.first < a.past; }
 
+// so many bytes (none at all: a box that meets no other)
+inline Box box_of(const void *data, int64_t bytes) {
+    Box b;
+    b.first = reinterpret_cast<uintptr_t>(data);
+    b.past = b.first + (uintptr_t)bytes;
+    b.fits = b.apart = b.past >= b.first;
+    return b;
+}
 inline Box box_of(const amap_heads &h, int64_t tokens, int dim) {
     const int64_t extent[3] = {tokens, h.heads, dim}, stride[3] = {h.token_stride, h.head_stride, 1};
     return box_of(h.data, bytes_of(h.type), 3, extent, stride);

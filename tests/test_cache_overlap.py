@@ -44,6 +44,25 @@ def test_queries_turned_in_place_between_other_strides(more):
     _refuses(B.AMAP_E_ALIAS, B.amap_cache_append, _cache(), _rows(6 * AT + HEAD, token=TOKEN), _rows(5 * AT), 10, 7 * AT, _rope(), 7 * AT, 0, q, q)
 
 
+def test_what_attend_writes():
+    """Caches of 8 pages, 4 requests in a table of 8 entries a row 10 apart, 2 heads of 64: out, lse and the workspace each within one another and whatever is read."""
+    need = B.amap_cache_attend_workspace(_cache(), 2, 4, 8)
+    size = dict(k=2 * 2048 * 8, v=2 * 2048 * 8, q=2 * 128 * 4, table=4 * 38, length=16, out=2 * 128 * 4, lse=4 * 8, work=need)
+    at = {n: (i + 2) * AT for i, n in enumerate(size)}
+
+    def call(at, type=B.AMAP_BF16, **over):
+        B.amap_cache_attend(_cache(k=at["k"], v=at["v"], type=type, **over), _rows(at["q"]), 4, at["table"], 10, 8, at["length"], 0.1, 0, _rows(at["out"]), at["lse"], at["work"], need)
+
+    for n in ("out", "lse", "work"):
+        for m in size:
+            if m != n:   # (the workspace begins at a multiple of 16; out at its first element)
+                for x in (at[m] + (size[m] - 4) // 16 * 16, at[m] - (size[n] - 4) // 16 * 16):
+                    _refuses(B.AMAP_E_ALIAS, call, {**at, n: x})
+        for scale in ("k_scale", "v_scale"):
+            _refuses(B.AMAP_E_ALIAS, lambda: call({**at, n: 12 * AT}, B.AMAP_E4M3, **{scale: 12 * AT}))
+    _refuses(B.AMAP_E_SHAPE, lambda: B.amap_cache_attend(_cache(), _rows(3 * AT), 1 << 29, 4 * AT, 1 << 40, 8, 5 * AT, 0.1, 0, _rows(6 * AT), None, 7 * AT, 1 << 40))
+
+
 # keys and values in one buffer; 8 pages of 16 tokens, 2 heads of 64, 2 bytes
 @pytest.mark.parametrize("over", [
     dict(v=AT + 2 * 64),                                                          # the second head of the keys is the first of the values
