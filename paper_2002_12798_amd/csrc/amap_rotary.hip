@@ -5,7 +5,7 @@
 // pairs, or a piece that holds whole pairs, or one that is only carried over), and the same one of up to U tokens: what it
 // is and where it lies are worked out once.  Its loads are issued first; while they are on their way the workgroup makes the tokens' angles, one
 // pair per lane, in LDS, where every head finds them: the angle is position x frequency in 64 bits, brought into one turn
-// there (at position 100 000 a 32-bit product is off by 4e-3 of a radian), its sine and cosine in 32.  Bound by the bytes of the rows: fp32
+// there (at position 100 000 a 32-bit product is off by 4e-3 of a radian), its sine and cosine in 32 by two parts of the angle.  Bound by the bytes of the rows: fp32
 // [65536, 16, 64] 90.6 us (537 MB, 5.9 TB/s), bf16 [12480, 16, 80] 16.1 us (64 MB; an identity copy 11.6), 16391 tokens of 32 + 2 x 8 heads of 128 with keys and values into 8
 // bits 71.8 us (369 MB; 58.8).  Four tokens of a lane: two 84 us, eight 94 us (their registers leave half the wavefronts) in the last case.
 #include "amap_cache.hpp"
@@ -220,10 +220,13 @@ __global__ __launch_bounds__(kMostThreads) void amap_turn_kernel(const TurnArgs 
                     position = a.position[axis_of(p) * a.axis_stride + t0 + t];
                     freq = a.freq[p];
                 }
-                const double turns = (double)position * (double)freq * 0.15915494309189533577;   // 1 / (2 pi)
+                const double turns = (double)position * (double)freq * 0.15915494309189533577, half = 2.0 * (turns - rint(turns));   // 1 / (2 pi)
                 float s, c;
-                sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-                angle[i] = make_float2(c, a.inverse ? -s : s);
+                const float most = (float)half, rest = (float)(half - (double)most) * 3.14159265358979323846f;
+                sincospif(most, &s, &c);
+                // (what rounding the angle left out, up to 9e-8 of a radian: as much as a step of the result, and all that there is of a sine next to a whole half turn)
+                const float sine = __builtin_fmaf(c, rest, s), cosine = __builtin_fmaf(-s, rest, c);
+                angle[i] = make_float2(cosine, a.inverse ? -sine : sine);
             }
             __syncthreads();
         }

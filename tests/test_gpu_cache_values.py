@@ -1,11 +1,12 @@
-"""What the operators around the paged cache give at values that an ordinary test does not meet: infinities among the visible values.  Needs an MI355X (-m gpu)."""
+"""What the operators around the paged cache give at values that an ordinary test does not meet: infinities among the visible values, angles whose sine or
+cosine is small.  Needs an MI355X (-m gpu)."""
 import math
 
 import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_cache import BF16, F16, HALF_STEP, SMALLEST, _close, _expect, _f64, _requests
+from tests.test_gpu_cache import BF16, F16, F32, HALF_STEP, SMALLEST, _close, _expect, _f64, _requests
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +73,25 @@ def test_values_that_became_infinite_in_the_store(dev):
     want = torch.zeros((1, 2, 64), device="cuda")
     want[..., 5], want[..., 7] = math.inf, -math.inf
     assert torch.equal(out.float(), want)
+
+
+# ---- the bits of an angle
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_where_a_sine_is_small(dev, interleaved):
+    """Angles next to whole quarters of a turn: what is left of them is small, and has to have the bits that the 64-bit angle has, not those of a fraction of
+    a turn in 32.  Sine and cosine at most 4 units of 2^-23 off (what OpenCL allows sinpi and cospi), the rest of the angle added by a product and a sum, the pair's
+    products by 0 and 1 exact: under 16 * 2^-24 of the value, and 2^-39 for 1600 radians in 64 bits (3 roundings of 2^-53 of them)."""
+    pairs, position = 512, 1000
+    quarters = torch.arange(pairs, dtype=torch.float64) * (math.pi / 2) / position
+    rope = dev.Rope(quarters.float().cuda(), None, interleaved)
+    x = torch.zeros((1, 2, 2 * pairs), dtype=F32, device="cuda")
+    first, second = (x[..., 0::2], x[..., 1::2]) if interleaved else (x[..., :pairs], x[..., pairs:])
+    first[:, 0], second[:, 1] = 1, 1
+    got = _f64(dev.rotary(x, rope, torch.tensor([position], dtype=torch.int32, device="cuda")))
+    angle = position * quarters.float().double().numpy()
+    c, s = np.cos(angle), np.sin(angle)
+    want = np.zeros((1, 2, 2 * pairs))
+    a, b = (want[..., 0::2], want[..., 1::2]) if interleaved else (want[..., :pairs], want[..., pairs:])
+    a[0, 0], b[0, 0], a[0, 1], b[0, 1] = c, s, -s, c
+    _close(got, want, 16 * 2.0 ** -24 * np.abs(want) + 2.0 ** -39)
