@@ -44,10 +44,12 @@ EXPORTS = [
 
 
 class AmapError(RuntimeError):
-    def __init__(self, status, what):
+    """`said`: whether the status is the library's, which then may have a reason for it (a refusal made here names its own in `what`)."""
+
+    def __init__(self, status, what, said=True):
         self.status = status
         detail = ""
-        if status == AMAP_E_HIP or (status == AMAP_E_UNSUPPORTED and what.startswith(("amap_gemm", "amap_execute", "amap_cache", "amap_rotary"))):
+        if said and (status == AMAP_E_HIP or (status == AMAP_E_UNSUPPORTED and what.startswith(("amap_gemm", "amap_execute", "amap_cache", "amap_rotary")))):
             detail = f" [{_L.amap_last_error().decode()}]"
         super().__init__(f"{what}: {_status_str(status)} (status {status}){detail}")
 

@@ -117,7 +117,7 @@ _capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", torch.cuda.is_c
 
 
 def _refused(what, why, status=B.AMAP_E_INVALID):
-    return B.AmapError(status, f"{what}: {why}")
+    return B.AmapError(status, f"{what}: {why}", said=False)
 
 
 def _on_gpu(t, dtype, rank, what, name):
