@@ -37,13 +37,14 @@ class PagedAttention:
         return device.gemm_fused(x.contiguous().view(torch.int16), m, w.view(torch.int16)).view(torch.bfloat16)
 
     def step(self, x, fresh):
-        """x [tokens, width]: the new tokens of request 0, of request 1, ... (fresh[r] of each).  -> each request's output at its newest token."""
+        """x [tokens, width]: the new tokens of request 0, of request 1, ... (fresh[r] of each).  -> each request's output at its newest token,
+        0 for a request that has no new one."""
         n, h, k = x.size(0), self.heads, self.kv_heads
         a = device.cache_assign(self.cache.page_size, self.length, fresh, self.table, self.free, n)
         qkv = self._product(x, [], self.w_qkv).view(n, h + 2 * k, self.dim)
         q = device.cache_append(self.cache, qkv[:, h:h + k], qkv[:, h + k:], a.slot, self.rope, a.position, qkv[:, :h])
-        newest = (a.begin[1:] - 1).long()
-        out, _ = device.cache_attend(self.cache, q[newest], self.table, a.length)
+        newest = (a.begin[1:] - 1).long().clamp(min=0)
+        out, _ = device.cache_attend(self.cache, q[newest], self.table, a.length * (fresh > 0))   # (without a new token that row is another request's query)
         self.length = a.length
         self.free = self.free[(torch.arange(self.free.numel(), device=x.device) + a.taken) % self.free.numel()]   # the pages behind those taken come first
         return self._product(out, [("reshape", (out.size(0), h * self.dim))], self.w_out)
