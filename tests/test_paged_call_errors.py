@@ -25,3 +25,27 @@ def test_that_refusal_for_a_tensor():
     with pytest.raises(B.AmapError) as e:
         device.rotary(x, device.Rope(torch.ones(32, device="cuda")), torch.zeros(4, dtype=torch.int32, device="cuda"))
     assert e.value.status == B.AMAP_E_UNSUPPORTED and "not contiguous" in str(e.value) and "2048" not in str(e.value)
+
+
+@pytest.mark.gpu
+def test_an_interrupt_passes_through_the_extension():
+    """Raised while it asks an object for its handle: an interrupt and an exit go on to the caller, any other error leaves the call to the way through ctypes."""
+    class Cache:
+        def __init__(self, error):
+            self.error, self.asked = error, 0
+
+        @property
+        def _cache_at(self):
+            self.asked += 1
+            raise self.error
+
+    x, slot = torch.zeros((1, 1, 8), device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    table, n = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for call in (lambda c: device._native.append(c, x, x, slot, None, None, None, None, None), lambda c: device._native.attend(c, x.half(), table, n, None, 0, None, None, None, None)):
+        for error in (KeyboardInterrupt, SystemExit):
+            cache = Cache(error())
+            with pytest.raises(error):
+                call(cache)
+            assert cache.asked == 1
+        cache = Cache(ValueError())
+        assert call(cache) is None and cache.asked == 1
