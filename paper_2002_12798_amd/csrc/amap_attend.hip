@@ -19,8 +19,8 @@
 //   An infinite value times a second part of 0 or of the other sign, or times a weight that has vanished in 32 bits, is NaN where the sum itself is infinite.  So a
 //     result that is not finite is looked at again: the same tiles with one weight, positive in both parts, for every score but -inf, and what is not finite then (infinite,
 //     or NaN of NaN, of both signs, or of an infinite score) takes the place of what was stored.  Whoever has no infinite values pays for the look: a multiply-add to a result.
-// Measured, cold: two requests of 131072 tokens, 32 queries to 8 key heads of 128, bf16 (1.07 GB) 181 us, 5.9 TB/s; 64 ragged ones up to 4096 (140 MB) 33.5 us, 28 of
-// them over shares and 5 of joining; 128 up to 2048 of an 8-bit cache, 12 heads of 64 (54 MB) 19 us; one of 500, 16 heads of 64, 6.5 us.
+// Measured, cold: two requests of 131072 tokens, 32 queries to 8 key heads of 128, bf16 (1.07 GB) 181 us, 5.9 TB/s; 64 ragged ones up to 4096 (140 MB) 33.8 us, 28 of
+// them over shares and 5 of joining; 128 up to 2048 of an 8-bit cache, 12 heads of 64 (54 MB) 19 us; one of 500, 16 heads of 64, 6.7 us.
 #include "amap_cache.hpp"
 
 #include <type_traits>
@@ -875,9 +875,10 @@ amap_status cut_of(const amap_cache &c, int heads, int64_t requests, int table_w
 
 // Wavefronts of a workgroup that has a segment to itself, or 0 for shares.  A compute unit by itself loads 52 bytes a ns, by four wavefronts as by eight (2000 tokens of 64,
 // one, two, four, eight of them: 44, 24.6, 15.1, 15.5 us), and the join of shares costs 4 to 6 us: so segments up to 288 KB (16 requests of 500 tokens, heads of 128, four to
-// a key head: 14.0 -> 11.0 us; four of 1000 tokens 12.4 by shares and 15.5), and 512 KB where all compute units have one (a window of 1000, 256 requests, heads of 96: 18.9 -> 13.3).  No more wavefronts
+// a key head: 14.0 -> 11.0 us; four of 1000 tokens 12.4 by shares and 15.5), and 512 KB where all compute units have one (a window of 1000, 256 requests, heads of 96: 18.9 -> 13.3, now 13.6).  No more wavefronts
 // than the chip holds at once (1600 segments of 500 tokens, one, two, three, four of them: 16.3, 14.7, 15.4, 17.7), and none with less than 32 KB.  A wavefront's
-// own part: up to 96 KB and 10 tiles (8 tiles of heads of 256, 32 KB each, by two wavefronts: 14.2 us, by shares 12.7).
+// own part: up to 96 KB and 10 tiles (8 tiles of heads of 256, 32 KB each, by two wavefronts: 14.2 us, by shares 12.7).  (These limits stand between the few points named here, the second
+// on the window alone; and the table says what a segment can be, not what it is: one request of 500 tokens, 16 heads of 64, 7.2 us in a table for 528 or 1024 and 9.5 in one for 4096 or 32768.)
 template <class F>
 uint32_t team_of(const AttendArgs &a) {
     uint32_t tiles = (a.most + kTokens - 1) / kTokens;   // of the longest segment that the table and the window allow: lengths are on the device

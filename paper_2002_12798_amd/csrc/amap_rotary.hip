@@ -136,7 +136,7 @@ __device__ __forceinline__ void store_as(uint32_t type, char *at, const float (&
 
 // How a pair's elements come to one lane: beside one another in one access (or nothing is turned); in two accesses, one to each half of the pairs; or in
 // two neighbouring lanes, one access each, which hand each other half of what they have.  The last covers rows without gaps where a half is no
-// whole number of 64-byte pieces (heads of 80, 40 pairs: 20.4 -> 15.2 us over 64 MB), and costs the others a little.
+// whole number of 64-byte pieces (heads of 80, 40 pairs: 20.4 -> 18.2 us over 64 MB when it was made, 16.1 now), and costs the others a little.
 enum Pairs { kBeside = 0, kHalves = 1, kLanes = 2 };
 
 // the neighbouring lane's

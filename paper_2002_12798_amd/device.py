@@ -255,7 +255,8 @@ def _made_on(stream):
 
 def cache_assign(page_size, cached, fresh, table, free_pages, n_tokens, out=None, stream=None) -> Assigned:
     """Pages, slots and positions for a step in which request r adds fresh[r] tokens to its cached[r] (None: none yet):
-    new pages are taken from the head of free_pages into `table`, which is changed in place.  All int32."""
+    new pages are taken from the head of free_pages into `table`, which is changed in place.  All int32.  What is made here is one buffer: whoever keeps one tensor of
+    it from step to step (`length`, which the next step has as `cached`) keeps the others' memory too, or a clone.  `out` may not hold what the call reads."""
     what = "amap_cache_assign"
     done = _native_assign(page_size, cached, fresh, table, free_pages, n_tokens, out, stream)
     if done is not None:
@@ -281,8 +282,8 @@ def cache_assign(page_size, cached, fresh, table, free_pages, n_tokens, out=None
 
 
 def rotary(x, rope, position, out=None, inverse=False, stream=None) -> torch.Tensor:
-    """out = x [tokens, heads, head_dim] turned to its positions ([tokens] or [axes, tokens], int32); inverse: turned back, the
-    gradient.  out may be x itself."""
+    """out = x [tokens, heads, head_dim] turned to its positions ([tokens] or [axes, tokens], int32); inverse: turned back.
+    out may be x itself.  No gradient is recorded, whatever x asks for: that of x is the output's, turned back."""
     what = "amap_rotary"
     done = _native_rotary(x, rope, position, out, inverse, stream)
     if done is not None:
@@ -328,7 +329,7 @@ def cache_append(cache, k, v, slot, rope=None, position=None, q=None, q_out=None
 def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=None, workspace=None, stream=None):
     """(out, lse): the attention of q [requests, heads, head_dim] over the first length[r] tokens (int32; window > 0: the last
     `window` of them) that table [requests, width] (int32) leads to.  scale: 1 / sqrt(head_dim) if None.  A request that sees nothing has
-    rows of 0 and lse -inf.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it; calls that may run at the same time, or
+    rows of 0 and lse -inf.  A visible value that is infinite or NaN counts as the formula has it.  No gradient is recorded.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it; calls that may run at the same time, or
     that two threads issue on one stream at the same time, must not be given the same one."""
     what = "amap_cache_attend"
     done = _native_attend(cache, q, table, length, scale, window, out, lse, workspace, stream)
