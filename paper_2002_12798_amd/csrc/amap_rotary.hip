@@ -90,11 +90,11 @@ __device__ __forceinline__ float widen<F16>(const char *at) {
     return (float)x;
 }
 
-// x / s, by whose reciprocal: rounded as the division is but for some last places (one correction of the product; a quotient that is
-// not finite has none)
+// x / s, by whose reciprocal: rounded as the division is but for some last places (one correction of the product; none where what is
+// left is not finite: the quotient is not, or the divisor)
 __device__ __forceinline__ float over(float x, float s, float reciprocal) {
     const float q = x * reciprocal, r = __builtin_fmaf(-q, s, x);
-    return __builtin_isfinite(q) ? __builtin_fmaf(r, reciprocal, q) : q;
+    return __builtin_isfinite(r) ? __builtin_fmaf(r, reciprocal, q) : q;
 }
 
 template <bool STREAM, class P>

@@ -75,6 +75,19 @@ def test_values_that_became_infinite_in_the_store(dev):
     assert torch.equal(out.float(), want)
 
 
+def test_scales_at_the_ends(dev):
+    """What is stored in an 8-bit cache is the value over its head's scale whatever that is: an infinite one, the smallest and the largest normal numbers, 0."""
+    scale = torch.tensor([math.inf, 2.0 ** -126, 2.0 ** 127, 0.0, -math.inf, 0.5], dtype=F32, device="cuda")
+    x = torch.tensor([0.0, 1.0, -3.5, 448.0, 2.0 ** -126, 2.0 ** 127, 3e38, math.inf, -math.inf, math.nan, 1e-3, -2.0 ** 120, 5.0, 6.0, 7.0, 2.0 ** 125], dtype=F32, device="cuda")
+    k, v = (torch.zeros((1, 1, 6, 16), dtype=torch.float8_e4m3fn, device="cuda") for _ in range(2))
+    rows = x.expand(1, 6, 16).contiguous()
+    dev.cache_append(dev.PagedCache(k, v, scale, scale), rows, rows, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    want = (rows.double() / scale.double()[:, None]).clamp(-448, 448)[0].cpu()   # (every quotient is a number of the type or far from a tie, or none)
+    got = k[0, 0].cpu()
+    assert torch.equal(got.view(torch.uint8), v[0, 0].cpu().view(torch.uint8)) and torch.equal(got.float().isnan(), want.isnan())
+    assert torch.equal(got.float().nan_to_num(0), want.to(torch.float8_e4m3fn).float().nan_to_num(0))
+
+
 # ---- the bits of an angle
 
 @pytest.mark.parametrize("interleaved", [False, True])
