@@ -329,8 +329,9 @@ def cache_append(cache, k, v, slot, rope=None, position=None, q=None, q_out=None
 def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=None, workspace=None, stream=None):
     """(out, lse): the attention of q [requests, heads, head_dim] over the first length[r] tokens (int32; window > 0: the last
     `window` of them) that table [requests, width] (int32) leads to.  scale: 1 / sqrt(head_dim) if None.  A request that sees nothing has
-    rows of 0 and lse -inf.  A visible value that is infinite or NaN counts as the formula has it.  No gradient is recorded.  workspace: a uint8 tensor of attend_workspace() bytes, for a program that keeps it; calls that may run at the same time, or
-    that two threads issue on one stream at the same time, must not be given the same one."""
+    rows of 0 and lse -inf; a visible value that is infinite or NaN counts as the formula has it.  No gradient is recorded.  workspace: a uint8 tensor
+    of attend_workspace() bytes, for a program that keeps it; calls that may run at the same time, or that two threads issue on one stream at the
+    same time, must not be given the same one."""
     what = "amap_cache_attend"
     done = _native_attend(cache, q, table, length, scale, window, out, lse, workspace, stream)
     if done is not None:
