@@ -27,6 +27,7 @@ KERNEL_NAMES = {0: "program", 1: "element", 2: "rows", 3: "tile", 4: "wave"}
 AMAP_MAX_RANK = 8
 AMAP_F32, AMAP_BF16, AMAP_F16, AMAP_E4M3 = range(4)
 AMAP_MAX_AXES = 4
+AMAP_SCALE_BLOCK = 128
 
 EXPORTS = [
     "amap_source", "amap_transpose", "amap_reshape", "amap_slice", "amap_repeat", "amap_tile", "amap_pad",
@@ -40,6 +41,7 @@ EXPORTS = [
     "amap_layout_create", "amap_layout_free", "amap_layout_tensor", "amap_layout_op", "amap_layout_solve",
     "amap_layout_order", "amap_layout_copy",
     "amap_cache_assign", "amap_rotary", "amap_cache_append", "amap_cache_attend", "amap_cache_attend_workspace",
+    "amap_norm", "amap_norm_grad", "amap_norm_grad_workspace", "amap_quantize", "amap_gemm_scaled",
 ]
 
 
@@ -49,7 +51,7 @@ class AmapError(RuntimeError):
     def __init__(self, status, what, said=True):
         self.status = status
         detail = ""
-        if said and (status == AMAP_E_HIP or (status == AMAP_E_UNSUPPORTED and what.startswith(("amap_gemm", "amap_execute", "amap_cache", "amap_rotary")))):
+        if said and (status == AMAP_E_HIP or (status == AMAP_E_UNSUPPORTED and what.startswith(("amap_gemm", "amap_execute", "amap_cache", "amap_rotary", "amap_norm", "amap_quantize")))):
             detail = f" [{_L.amap_last_error().decode()}]"
         super().__init__(f"{what}: {_status_str(status)} (status {status}){detail}")
 
@@ -497,13 +499,27 @@ class amap_assign(C.Structure):
                 ("position", _vp), ("owner", _vp), ("n_tokens", C.c_int64), ("taken", _vp)]
 
 
+class amap_rows(C.Structure):
+    _fields_ = [("data", _vp), ("type", C.c_int), ("row_stride", C.c_int64)]
+
+
+class amap_scales(C.Structure):
+    _fields_ = [("data", _vp), ("row_stride", C.c_int64), ("block_stride", C.c_int64)]
+
+
 _heads_p, _rope_p, _cache_p = C.POINTER(amap_heads), C.POINTER(amap_rope), C.POINTER(amap_cache)
+_rows_p, _scales_p = C.POINTER(amap_rows), C.POINTER(amap_scales)
 for _name, _types in (
         ("amap_cache_assign", [C.POINTER(amap_assign), _vp]),
         ("amap_rotary", [_heads_p, _heads_p, C.c_int64, C.c_int, _rope_p, _vp, C.c_int64, C.c_int, _vp]),
         ("amap_cache_append", [_cache_p, _heads_p, _heads_p, C.c_int64, _vp, _rope_p, _vp, C.c_int64, _heads_p, _heads_p, _vp]),
         ("amap_cache_attend", [_cache_p, _heads_p, C.c_int64, _vp, C.c_int64, C.c_int, _vp, C.c_float, C.c_int, _heads_p, _vp, _vp, C.c_int64, _vp]),
-        ("amap_cache_attend_workspace", [_cache_p, C.c_int, C.c_int64, C.c_int, _i64p])):
+        ("amap_cache_attend_workspace", [_cache_p, C.c_int, C.c_int64, C.c_int, _i64p]),
+        ("amap_norm", [_heads_p, _heads_p, C.c_int64, C.c_int, _vp, C.c_int, C.c_float, _heads_p, _heads_p, _scales_p, _vp]),
+        ("amap_norm_grad", [_heads_p, C.c_int64, C.c_int, _vp, C.c_int, C.c_float, _heads_p, _heads_p, _heads_p, _vp, _vp, C.c_int64, _vp]),
+        ("amap_norm_grad_workspace", [C.c_int, C.c_int64, C.c_int, C.c_int, _i64p]),
+        ("amap_quantize", [_rows_p, _rows_p, C.c_int64, C.c_int64, C.c_int, _rows_p, _scales_p, _vp]),
+        ("amap_gemm_scaled", [_rows_p, _scales_p, _rows_p, _scales_p, C.c_int64, C.c_int64, C.c_int64, _rows_p, _vp])):
     if hasattr(_L, _name):   # (a build of the host logic alone has none of these)
         getattr(_L, _name).argtypes = _types
 
@@ -532,6 +548,29 @@ def amap_cache_attend_workspace(cache, heads, requests, table_width):
 def amap_cache_attend(cache, q, requests, table_ptr, table_stride, table_width, length_ptr, scale, window, out, lse_ptr, workspace_ptr, workspace_bytes, stream=0):
     _check(_L.amap_cache_attend(cache, q, int(requests), _addr(table_ptr), int(table_stride), int(table_width), _addr(length_ptr), float(scale), int(window),
                                 out, _addr(lse_ptr), _addr(workspace_ptr), int(workspace_bytes), _addr(stream)), "amap_cache_attend")
+
+
+def amap_norm(x, residual, tokens, head_dim, weight_ptr, weight_type, eps, total, out, scale=None, stream=0):
+    _check(_L.amap_norm(x, residual, int(tokens), int(head_dim), _addr(weight_ptr), int(weight_type), float(eps), total, out, scale, _addr(stream)), "amap_norm")
+
+
+def amap_norm_grad_workspace(heads, tokens, head_dim, type):
+    n = C.c_int64()
+    _check(_L.amap_norm_grad_workspace(int(heads), int(tokens), int(head_dim), int(type), C.byref(n)), "amap_norm_grad_workspace")
+    return n.value
+
+
+def amap_norm_grad(x, tokens, head_dim, weight_ptr, weight_type, eps, grad, extra, dx, dweight_ptr, workspace_ptr=None, workspace_bytes=0, stream=0):
+    _check(_L.amap_norm_grad(x, int(tokens), int(head_dim), _addr(weight_ptr), int(weight_type), float(eps), grad, extra, dx, _addr(dweight_ptr),
+                             _addr(workspace_ptr), int(workspace_bytes), _addr(stream)), "amap_norm_grad")
+
+
+def amap_quantize(x, gate, rows, columns, tall, out, scale, stream=0):
+    _check(_L.amap_quantize(x, gate, int(rows), int(columns), int(tall), out, scale, _addr(stream)), "amap_quantize")
+
+
+def amap_gemm_scaled(a, a_scale, w, w_scale, m, n, k, out, stream=0):
+    _check(_L.amap_gemm_scaled(a, a_scale, w, w_scale, int(m), int(n), int(k), out, _addr(stream)), "amap_gemm_scaled")
 
 
 class GraphDME:

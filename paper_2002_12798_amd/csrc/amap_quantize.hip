@@ -1,0 +1,162 @@
+// Rows and weights into 8 bits with a scale for each block (amap_quantize): every block is read once, held in registers while the lanes that hold it
+// agree on its largest value, and written once.  Bound by the bytes.
+#include "amap_rows.hpp"
+
+using namespace amap_rows_detail;
+using namespace amap_detail;
+using namespace amap_dev;
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct QuantizeArgs {
+    const char *x, *gate;
+    char *out;
+    float *scale;
+    int64_t x_row, gate_row, out_row;   // bytes
+    int64_t scale_row, scale_block;
+    uint32_t rows, columns, across;     // across: workgroups along a row
+    FastDiv by_across;
+};
+
+// gate / (1 + exp(-gate)), by exp(-|gate|): neither overflows nor loses what is small.  The product with 1 / ln 2 is carried in two parts, so that the power of two
+// has 32 bits whatever the gate.
+__device__ __forceinline__ float gated(float gate) {
+    const float a = -__builtin_fabsf(gate), t = a * 0x1.715476p+0f;
+    const float rest = __builtin_fmaf(a, 0x1.715476p+0f, -t) + a * 0x1.4ae0bf8p-26f;
+    float e = __builtin_amdgcn_exp2f(t);
+    e = __builtin_fmaf(e, rest * 0x1.62e43p-1f, e);
+    return gate * (gate < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+}
+
+// Blocks of one row: a block to as many lanes as it has pieces, U blocks beside one another for each of them; the rows of a workgroup follow one another, so that
+// the scales of a column of blocks are written beside one another.
+template <class T, bool GATE, int U>
+__global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeArgs a) {
+    constexpr int V = kPer<T>, L = kBlockLanes<T>;
+    constexpr uint32_t kRows = kThreads / L;
+    const uint32_t down = fdiv(blockIdx.x, a.by_across), across = blockIdx.x - down * a.across;
+    const uint32_t lane = threadIdx.x % L, row = down * kRows + threadIdx.x / L;
+    if (row >= a.rows) return;   // (whole groups of lanes)
+    // (from the workgroup's first column on)
+    const uint32_t column = across * (U * kBlock), left = min(a.columns - column, (uint32_t)(U * kBlock)), first = lane * V;
+    const char *const x = a.x + row * a.x_row + (size_t)column * T::bytes, *const gate = GATE ? a.gate + row * a.gate_row + (size_t)column * T::bytes : nullptr;
+    char *const out = a.out + row * a.out_row + column;
+    u32x4 p[U], q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        p[u] = load_piece<T>(x, first + u * kBlock, left);
+        if constexpr (GATE) q[u] = load_piece<T>(gate, first + u * kBlock, left);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t at = first + u * kBlock;
+        float y[V], most = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            y[e] = element<T>(p[u], e);
+            if constexpr (GATE) y[e] *= gated(element<T>(q[u], e));
+            most = fmaxf(most, size_of(y[e]));
+        }
+        const float scale = scale_of(most_over<L>(most));
+        uint32_t word[V / 4];
+        eight_bits<V>(y, reciprocal_of(scale), word);
+        store_eight<V>(out, at, left, word);
+        if (lane == 0 && at < left) a.scale[row * a.scale_row + (int64_t)(across * U + u) * a.scale_block] = scale;
+    }
+}
+
+// Blocks of 128 rows: one to a workgroup.
+template <class T>
+__global__ __launch_bounds__(kThreads) void amap_quantize_tall_kernel(const QuantizeArgs a) {
+    constexpr int V = kPer<T>, L = kBlockLanes<T>, kRows = kThreads / L, U = kBlock / kRows;
+    __shared__ float part[kThreads / 64];
+    const uint32_t down = fdiv(blockIdx.x, a.by_across), across = blockIdx.x - down * a.across;
+    const uint32_t column = across * kBlock, left = min(a.columns - column, (uint32_t)kBlock), at = threadIdx.x % L * V, first = down * kBlock + threadIdx.x / L;
+    const char *const x = a.x + (size_t)column * T::bytes;
+    u32x4 p[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t row = first + u * kRows;
+        p[u] = load_piece<T>(x + row * a.x_row, row < a.rows ? at : left, left);
+    }
+    float most = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) most = fmaxf(most, size_of(element<T>(p[u], e)));
+    most = most_over<64>(most);
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) most = fmaxf(most, part[w]);
+    const float scale = scale_of(most), by = reciprocal_of(scale);
+    if (threadIdx.x == 0) a.scale[down * a.scale_row + across * a.scale_block] = scale;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t row = first + u * kRows;
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = element<T>(p[u], e);
+        uint32_t word[V / 4];
+        eight_bits<V>(y, by, word);
+        if (row < a.rows) store_eight<V>(a.out + column + row * a.out_row, at, left, word);
+    }
+}
+
+template <class T>
+hipError_t quantize_of(QuantizeArgs &g, int tall, hipStream_t s, bool &fits) {
+    const uint64_t blocks = (uint64_t)blocks_of(g.columns);
+    uint64_t each = 1, rows = kBlock;
+    if (tall == 1) {
+        rows = kThreads / kBlockLanes<T>;
+        each = g.gate ? 2 : 4;   // blocks of a lane: as many while that leaves every compute unit four workgroups
+        while (each > 1 && ((blocks + each - 1) / each) * ((g.rows + rows - 1) / rows) < 1024) each /= 2;
+    }
+    g.across = (uint32_t)((blocks + each - 1) / each);
+    g.by_across = make_fastdiv(g.across);
+    const uint64_t grid = g.across * (((uint64_t)g.rows + rows - 1) / rows);
+    fits = grid < (1u << 24);   // (threads of a launch: 32 bits)
+    if (!fits) return hipSuccess;
+    const dim3 at((uint32_t)grid), threads(kThreads);
+    if (tall != 1) return launch_kernel<amap_quantize_tall_kernel<T>>(at, threads, 0, s, g);
+    if (g.gate) return each == 2 ? launch_kernel<amap_quantize_kernel<T, true, 2>>(at, threads, 0, s, g) : launch_kernel<amap_quantize_kernel<T, true, 1>>(at, threads, 0, s, g);
+    if (each == 4) return launch_kernel<amap_quantize_kernel<T, false, 4>>(at, threads, 0, s, g);
+    return each == 2 ? launch_kernel<amap_quantize_kernel<T, false, 2>>(at, threads, 0, s, g) : launch_kernel<amap_quantize_kernel<T, false, 1>>(at, threads, 0, s, g);
+}
+
+}  // namespace
+
+extern "C" amap_status amap_quantize(const amap_rows *x, const amap_rows *gate, int64_t rows, int64_t columns, int tall, const amap_rows *out, const amap_scales *scale,
+                                     void *stream) {
+    if (!x || !out || !scale || rows < 0 || columns < 0 || !is_wide(x->type) || out->type != AMAP_E4M3 || (gate && gate->type != x->type)) return AMAP_E_INVALID;
+    if (tall != 1 && tall != kBlock) return refuse("blocks of other than 1 or 128 rows");
+    if (gate && tall != 1) return refuse("a gate in front of blocks of 128 rows");
+    if (rows > INT32_MAX || columns > INT32_MAX) return AMAP_E_SHAPE;
+    if (rows == 0 || columns == 0) return AMAP_OK;
+    if (!x->data || !out->data || !scale->data || (gate && !gate->data)) return AMAP_E_INVALID;
+    const Box from = amap_rows_detail::box_of(*x, rows, columns), by = gate ? amap_rows_detail::box_of(*gate, rows, columns) : Box{},
+              to = amap_rows_detail::box_of(*out, rows, columns), sc = amap_rows_detail::box_of(*scale, (rows + tall - 1) / tall, blocks_of(columns));
+    if (!from.fits || (gate && !by.fits) || !to.fits || !to.apart || !sc.fits || !sc.apart) return AMAP_E_SHAPE;
+    if (meet(to, from) || meet(to, by) || meet(sc, from) || meet(sc, by) || meet(sc, to)) return AMAP_E_ALIAS;
+    const int es = bytes_of(x->type);
+    if (reinterpret_cast<uintptr_t>(x->data) % es || (gate && reinterpret_cast<uintptr_t>(gate->data) % es) || reinterpret_cast<uintptr_t>(scale->data) % 4)
+        return refuse("a tensor that does not begin at a whole element");
+    QuantizeArgs g = {};
+    g.x = static_cast<const char *>(x->data);
+    g.x_row = x->row_stride * es;
+    if (gate) g.gate = static_cast<const char *>(gate->data), g.gate_row = gate->row_stride * es;
+    g.out = static_cast<char *>(out->data);
+    g.out_row = out->row_stride;
+    g.scale = scale->data;
+    g.scale_row = scale->row_stride, g.scale_block = scale->block_stride;
+    g.rows = (uint32_t)rows;
+    g.columns = (uint32_t)columns;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const StreamDevice device(s);
+    if (device.status() != hipSuccess) return launched(device.status(), "the stream's device");
+    bool fits;
+    const hipError_t e = x->type == AMAP_F32 ? quantize_of<F32>(g, tall, s, fits) : x->type == AMAP_BF16 ? quantize_of<Bf16>(g, tall, s, fits) : quantize_of<F16>(g, tall, s, fits);
+    return fits ? launched(e, "amap_quantize_kernel") : refuse("too many blocks for one launch");
+}

@@ -366,3 +366,169 @@ def cache_attend(cache, q, table, length, scale=None, window=0, out=None, lse=No
 def attend_workspace(cache, heads, requests, table_width) -> int:
     """Bytes of workspace that cache_attend takes for such a call."""
     return B.amap_cache_attend_workspace(cache._c, heads, requests, table_width)
+
+
+# ---- a layer's rows in 8 bits: the norm in front of a product, rows and weights with a scale for each block of 128, the product of them
+
+class Normed(NamedTuple):
+    out: torch.Tensor                # the norm, in x's type or (eight) float8_e4m3fn
+    scale: torch.Tensor | None       # eight: [tokens, ceil(dim / 128)] float32
+    total: torch.Tensor | None       # with a residual: x + residual
+
+
+class Eight(NamedTuple):
+    out: torch.Tensor                # [rows, columns] float8_e4m3fn
+    scale: torch.Tensor              # [ceil(rows / tall), ceil(columns / 128)] float32
+
+
+def _blocks(n):
+    return -(-n // B.AMAP_SCALE_BLOCK)
+
+
+def _made_scales(rows, blocks, beside):
+    """Scales as the product likes to read them: those of one block of columns beside one another."""
+    return torch.empty((blocks, rows), dtype=torch.float32, device=beside.device).t()
+
+
+def _heads_or_rows(t, what, name, like=None, dtype=None):
+    """A [tokens, heads, dim] or [tokens, dim] tensor as the library takes it; `like`: of the same shape (and type, unless another one is named)."""
+    if not isinstance(t, torch.Tensor) or t.dim() not in (2, 3) or t.dtype not in _ELEMENT:
+        raise _refused(what, f"{name} is no tensor of 2 or 3 dimensions and a known type")
+    if like is not None and t.shape != like.shape:
+        raise _refused(what, f"{name} is {tuple(t.shape)}, not {tuple(like.shape)}", B.AMAP_E_SHAPE)
+    want = dtype if dtype is not None else t.dtype if like is None else like.dtype
+    if _ELEMENT[t.dtype] != _ELEMENT[want]:
+        raise _refused(what, f"{name} is of {t.dtype}, not of {want}")
+    _on_gpu(t, t.dtype, t.dim(), what, name)
+    if t.dim() == 3:
+        return B.amap_heads(t.data_ptr(), _ELEMENT[t.dtype], t.size(1), t.stride(0), t.stride(1))
+    return B.amap_heads(t.data_ptr(), _ELEMENT[t.dtype], 1, t.stride(0), 0)
+
+
+def _matrix(t, what, name):
+    if not isinstance(t, torch.Tensor) or t.dtype not in _ELEMENT:
+        raise _refused(what, f"{name} is no tensor of a known type")
+    _on_gpu(t, t.dtype, 2, what, name)
+    return B.amap_rows(t.data_ptr(), _ELEMENT[t.dtype], t.stride(0))
+
+
+def _scales(t, rows, blocks, what, name):
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.dim() != 2:
+        raise _refused(what, f"{name} is no torch.float32 tensor of 2 dimensions")
+    if not t.is_cuda:
+        raise _refused(what, f"{name} is not on the GPU")
+    if tuple(t.shape) != (rows, blocks):
+        raise _refused(what, f"{name} is {tuple(t.shape)}, not {(rows, blocks)}", B.AMAP_E_SHAPE)
+    return B.amap_scales(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _norm_weight(weight, x, what):
+    if not isinstance(weight, torch.Tensor) or weight.dtype not in (x.dtype, torch.float32):
+        raise _refused(what, f"weight is no tensor of {x.dtype} or torch.float32")
+    if _on_gpu(weight, weight.dtype, 1, what, "weight").size(0) != x.size(-1):
+        raise _refused(what, f"weight holds {weight.size(0)} elements, not {x.size(-1)}", B.AMAP_E_SHAPE)
+    return weight.data_ptr(), _ELEMENT[weight.dtype]
+
+
+def norm(x, weight, eps=1e-6, residual=None, eight=False, out=None, scale=None, total=None, stream=None) -> Normed:
+    """The root mean square norm of x [tokens, dim] or [tokens, heads, dim] (each head by itself), times weight [dim] (x's type or float32): with a residual, of
+    total = x + residual, rounded to their type.  eight: out in float8_e4m3fn with a scale for each row's blocks of 128 (x [tokens, dim] only).
+    out and total may each be x or residual themselves.  No gradient is recorded: norm_grad makes it."""
+    what = "amap_norm"
+    a = _heads_or_rows(x, what, "x")
+    if x.dtype == torch.float8_e4m3fn or (eight and x.dim() != 2) or (scale is not None and not eight) or (total is not None and residual is None):
+        raise _refused(what, "x of 8 bits" if x.dtype == torch.float8_e4m3fn else "eight is for x [tokens, dim]" if eight and x.dim() != 2 else
+                       "a scale without eight" if scale is not None else "a total without a residual")
+    dim, of = x.size(-1), torch.float8_e4m3fn if eight else x.dtype
+    b = None if residual is None else _heads_or_rows(residual, what, "residual", x)
+    at, kind = _norm_weight(weight, x, what)
+    with _made_on(stream):
+        if out is None:
+            out = torch.empty(x.shape, dtype=of, device=x.device)
+        if eight and scale is None:
+            scale = _made_scales(x.size(0), _blocks(dim), x)
+        if residual is not None and total is None:
+            total = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    d = _heads_or_rows(out, what, "out", x, of)
+    s = None if scale is None else _scales(scale, x.size(0), _blocks(dim), what, "scale")
+    t = None if total is None else _heads_or_rows(total, what, "total", x)
+    B.amap_norm(a, b, x.size(0), dim, at, kind, eps, t, d, s, current_stream() if stream is None else stream)
+    return Normed(out, scale, total)
+
+
+def norm_grad(x, weight, grad, eps=1e-6, extra=None, dx=None, dweight=None, workspace=None, stream=None):
+    """(dx, dweight): the gradient of norm(x, weight) (with a residual: of its total) from that of its output, all of x's shape and type; extra: what reaches x by
+    other ways, added to dx.  dweight [dim] is float32, and the same at every call.  dx may be x, grad or extra themselves.  workspace: a uint8 tensor of
+    norm_grad_workspace() bytes, for a program that keeps it; calls that may run at the same time must not be given the same one."""
+    what = "amap_norm_grad"
+    a = _heads_or_rows(x, what, "x")
+    if x.dtype == torch.float8_e4m3fn:
+        raise _refused(what, "x of 8 bits")
+    b = _heads_or_rows(grad, what, "grad", x)
+    c = None if extra is None else _heads_or_rows(extra, what, "extra", x)
+    at, kind = _norm_weight(weight, x, what)
+    need = norm_grad_workspace(x)
+    with _made_on(stream):
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if dweight is None:
+            dweight = torch.empty(x.size(-1), dtype=torch.float32, device=x.device)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    d = _heads_or_rows(dx, what, "dx", x)
+    if _on_gpu(dweight, torch.float32, 1, what, "dweight").size(0) != x.size(-1):
+        raise _refused(what, f"dweight holds {dweight.size(0)} elements, not {x.size(-1)}", B.AMAP_E_SHAPE)
+    have = 0 if workspace is None else _on_gpu(workspace, torch.uint8, 1, what, "workspace").numel()
+    B.amap_norm_grad(a, x.size(0), x.size(-1), at, kind, eps, b, c, d, dweight.data_ptr(), None if workspace is None else workspace.data_ptr(), have,
+                     current_stream() if stream is None else stream)
+    return dx, dweight
+
+
+def norm_grad_workspace(x) -> int:
+    """Bytes of workspace that norm_grad takes for such rows."""
+    return B.amap_norm_grad_workspace(x.size(1) if x.dim() == 3 else 1, x.size(0), x.size(-1), _ELEMENT[x.dtype])
+
+
+def quantize(x, gate=None, tall=1, out=None, scale=None, stream=None) -> Eight:
+    """x [rows, columns] in float8_e4m3fn, with a float32 scale for each block of `tall` (1: activations, 128: weights) rows and 128 columns: the block's largest value over
+    448.  gate: silu(gate) * x instead (tall 1)."""
+    what = "amap_quantize"
+    a = _matrix(x, what, "x")
+    b = None if gate is None else _matrix(gate, what, "gate")
+    if gate is not None and gate.shape != x.shape:
+        raise _refused(what, f"gate is {tuple(gate.shape)}, not {tuple(x.shape)}", B.AMAP_E_SHAPE)
+    if tall not in (1, B.AMAP_SCALE_BLOCK):
+        raise _refused(what, f"blocks of {tall} rows, not of 1 or 128", B.AMAP_E_UNSUPPORTED)
+    rows, columns = x.shape
+    with _made_on(stream):
+        if out is None:
+            out = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+        if scale is None:
+            scale = _made_scales(-(-rows // tall), _blocks(columns), x)
+    c = _matrix(out, what, "out")
+    if out.shape != x.shape:
+        raise _refused(what, f"out is {tuple(out.shape)}, not {tuple(x.shape)}", B.AMAP_E_SHAPE)
+    B.amap_quantize(a, b, rows, columns, tall, c, _scales(scale, -(-rows // tall), _blocks(columns), what, "scale"), current_stream() if stream is None else stream)
+    return Eight(out, scale)
+
+
+def gemm_scaled(a, a_scale, w, w_scale, dtype=torch.bfloat16, out=None, stream=None) -> torch.Tensor:
+    """a [m, k] times w [n, k] transposed, both float8_e4m3fn with the scales that quantize gives (a: tall 1, w: tall 128), summed in 32 bits and rounded once to
+    dtype (bfloat16, float16, float32; out's type if there is one).  k is a multiple of 16, and rows begin at multiples of 16 bytes."""
+    what = "amap_gemm_scaled"
+    x, y = _matrix(a, what, "a"), _matrix(w, what, "w")
+    m, k = a.shape
+    n = w.size(0)
+    if w.size(1) != k:
+        raise _refused(what, f"a and w have {k} and {w.size(1)} columns", B.AMAP_E_SHAPE)
+    s, t = _scales(a_scale, m, _blocks(k), what, "a_scale"), _scales(w_scale, _blocks(n), _blocks(k), what, "w_scale")
+    if out is None:
+        if dtype not in (torch.bfloat16, torch.float16, torch.float32):
+            raise _refused(what, f"a product in {dtype}")
+        with _made_on(stream):
+            out = torch.empty((m, n), dtype=dtype, device=a.device)
+    z = _matrix(out, what, "out")
+    if tuple(out.shape) != (m, n):
+        raise _refused(what, f"out is {tuple(out.shape)}, not {(m, n)}", B.AMAP_E_SHAPE)
+    B.amap_gemm_scaled(x, s, y, t, m, n, k, z, current_stream() if stream is None else stream)
+    return out
