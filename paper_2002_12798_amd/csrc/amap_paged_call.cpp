@@ -1,4 +1,4 @@
-// The way from a Python call to the operators around the paged cache: torch's tensors taken as they are, outputs made, one call of a C entry point.
+// The way from a Python call to the operators around the paged cache and on a layer's rows in 8 bits: torch's tensors taken as they are, outputs made, one call of a C entry point.
 //
 // These calls run for 4 to 10 us on the GPU where requests are few, and issuing a launch takes 3.5 of them; asked for through the interpreter, a tensor's
 // type, shape, strides and address are 0.3 us, a new tensor is 1.7.  Here they are 0.01 and 0.5.  Only the ordinary call is taken:
@@ -7,6 +7,7 @@
 // one torch, whose objects it looks into: another one is told apart by its version, and does without.
 #include <ATen/ATen.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <pthread.h>
@@ -22,6 +23,12 @@ decltype(&amap_rotary) p_rotary;
 decltype(&amap_cache_append) p_append;
 decltype(&amap_cache_attend) p_attend;
 decltype(&amap_cache_attend_workspace) p_room;
+decltype(&amap_norm) p_norm;
+decltype(&amap_norm_grad) p_norm_grad;
+decltype(&amap_norm_grad_workspace) p_norm_grad_room;
+decltype(&amap_quantize) p_quantize;
+decltype(&amap_gemm_scaled) p_gemm_scaled;
+PyObject *normed, *in_eight;   // the types of their answers
 PyObject *raw_stream, *get_device, *is_initialized, *is_capturing, *s_cache_at, *s_rope_at, *s_work, *assigned;
 bool initialized;   // torch said so in this process (a fork asks again)
 
@@ -351,6 +358,204 @@ PyObject *assign(PyObject *const *a, Py_ssize_t n) {
     return result(called([&] { return p_assign(&g, stream); }), again(out.o));
 }
 
+// ---- a layer's rows in 8 bits
+
+bool type_of(at::ScalarType t, amap_type &type) {
+    switch (t) {
+    case at::kFloat: type = AMAP_F32; return true;
+    case at::kBFloat16: type = AMAP_BF16; return true;
+    case at::kHalf: type = AMAP_F16; return true;
+    case at::kFloat8_e4m3fn: type = AMAP_E4M3; return true;
+    default: return false;
+    }
+}
+// [tokens, heads, dim] or [tokens, dim], of x's shape and type if there is one
+const at::Tensor *like_rows(PyObject *o, amap_heads &h, const at::Tensor *x = nullptr) {
+    if (!THPVariable_Check(o)) return nullptr;
+    const int64_t rank = THPVariable_Unpack(o).dim();
+    const at::Tensor *const t = rank == 2 || rank == 3 ? tensor(o, (int)rank) : nullptr;
+    if (!t || !type_of(t->scalar_type(), h.type) || t->size(rank - 1) > INT32_MAX || (rank == 3 && t->size(1) > INT32_MAX)) return nullptr;
+    if (x && (t->sizes() != x->sizes() || t->device() != x->device())) return nullptr;
+    h.data = data<void>(*t);
+    h.heads = rank == 3 ? (int)t->size(1) : 1;
+    h.token_stride = t->stride(0);
+    h.head_stride = rank == 3 ? t->stride(1) : 0;
+    return t;
+}
+const at::Tensor *matrix(PyObject *o, amap_rows &r, const at::Tensor *beside = nullptr) {
+    const at::Tensor *const t = tensor(o, 2);
+    if (!t || !type_of(t->scalar_type(), r.type) || (beside && t->device() != beside->device())) return nullptr;
+    r.data = data<void>(*t);
+    r.row_stride = t->stride(0);
+    return t;
+}
+bool scales(PyObject *o, int64_t rows, int64_t blocks, const at::Tensor &beside, amap_scales &s) {
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || t.layout() != at::kStrided || t.device() != beside.device() || t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != rows || t.size(1) != blocks)
+        return false;
+    s.data = data<float>(t);
+    s.row_stride = t.stride(0);
+    s.block_stride = t.stride(1);
+    return true;
+}
+int64_t blocks_of(int64_t n) { return (n + AMAP_SCALE_BLOCK - 1) / AMAP_SCALE_BLOCK; }
+// The stream of a call on tensors beside this one: a current stream belongs to the current device.
+bool stream_beside(PyObject *o, const at::Tensor &t, void **stream) {
+    if (!stream_of(o, stream)) return false;
+    if (o != Py_None) return true;
+    Ref dev(PyObject_CallNoArgs(get_device));
+    int64_t n;
+    return dev.o && whole(dev.o, t.get_device(), t.get_device(), &n);
+}
+// A norm's weight [dim]: of the rows' type or 32 bits
+const at::Tensor *weight_of(PyObject *o, const at::Tensor &x, amap_type &type) {
+    const at::Tensor *const t = tensor(o, 1);
+    if (!t || !type_of(t->scalar_type(), type) || (t->scalar_type() != at::kFloat && t->scalar_type() != x.scalar_type())) return nullptr;
+    return t->size(0) == x.size(x.dim() - 1) && t->device() == x.device() ? t : nullptr;
+}
+// 8-bit rows and their scales, those of one block of columns beside one another, in one allocation
+void make_eight(const at::Tensor &beside, at::IntArrayRef size, int64_t scale_rows, Ref &out, Ref &scale) {
+    const int64_t rows = size[0], columns = size[1], blocks = blocks_of(columns), behind = (rows * columns + 15) / 16 * 4;
+    const at::Tensor words = made({behind + scale_rows * blocks}, beside, at::kInt);
+    out.o = THPVariable_Wrap(part(words, at::kFloat8_e4m3fn, size, 0));
+    at::Tensor s = part(words, at::kFloat, {scale_rows, blocks}, behind);
+    const int64_t shape[2] = {scale_rows, blocks}, stride[2] = {1, scale_rows < 1 ? 1 : scale_rows};
+    s.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef(shape, 2), at::IntArrayRef(stride, 2));
+    scale.o = THPVariable_Wrap(std::move(s));
+}
+PyObject *named(PyObject *type, PyObject *const *fields, int n) {   // of a named tuple type
+    Ref all(PyTuple_New(n));
+    if (!all.o) return nullptr;
+    for (int i = 0; i < n; ++i) PyTuple_SET_ITEM(all.o, i, again(fields[i]));
+    Ref args(PyTuple_Pack(1, all.o));
+    return args.o ? PyTuple_Type.tp_new(reinterpret_cast<PyTypeObject *>(type), args.o, nullptr) : nullptr;
+}
+
+// norm(x, weight, eps, residual or None, eight, out or None, scale or None, total or None, stream or None) -> (out, scale, total)
+PyObject *norm(PyObject *const *a, Py_ssize_t n) {
+    amap_heads x, residual, total, out;
+    amap_scales s;
+    amap_type kind;
+    void *stream;
+    if (n != 9 || !p_norm || !PyFloat_CheckExact(a[2]) || !PyBool_Check(a[4])) return nullptr;
+    const at::Tensor *const tx = like_rows(a[0], x), *const tw = tx ? weight_of(a[1], *tx, kind) : nullptr;
+    const bool eight = a[4] == Py_True, added = a[3] != Py_None;
+    if (!tw || x.type == AMAP_E4M3 || (eight && tx->dim() != 2) || (!eight && a[6] != Py_None) || (!added && a[7] != Py_None)) return nullptr;
+    if (eight && (a[5] == Py_None) != (a[6] == Py_None)) return nullptr;
+    const bool make_total = added && a[7] == Py_None;
+    if (((a[5] == Py_None || make_total) && a[8] != Py_None) || !stream_beside(a[8], *tx, &stream)) return nullptr;
+    if (added && (!like_rows(a[3], residual, tx) || residual.type != x.type)) return nullptr;
+    Ref o, sc(again(Py_None)), t(again(Py_None));
+    {
+        Making without;
+        if (a[5] != Py_None) {
+            o.o = again(a[5]);
+            Py_SETREF(sc.o, again(a[6]));
+        } else if (eight) {
+            Py_CLEAR(sc.o);
+            make_eight(*tx, tx->sizes(), tx->size(0), o, sc);
+        } else {
+            o.o = THPVariable_Wrap(made(tx->sizes(), *tx, tx->scalar_type()));
+        }
+        if (added) Py_SETREF(t.o, make_total ? THPVariable_Wrap(made(tx->sizes(), *tx, tx->scalar_type())) : again(a[7]));
+    }
+    const int64_t tokens = tx->size(0);
+    const int dim = (int)tx->size(tx->dim() - 1);
+    if (!o.o || !sc.o || !t.o || !like_rows(o.o, out, tx) || out.type != (eight ? AMAP_E4M3 : x.type) || (added && !like_rows(t.o, total, tx))) return nullptr;
+    if (eight && !scales(sc.o, tokens, blocks_of(dim), *tx, s)) return nullptr;
+    const void *const weight = data<void>(*tw);
+    const float eps = (float)PyFloat_AS_DOUBLE(a[2]);
+    const amap_status st = called([&] { return p_norm(&x, added ? &residual : nullptr, tokens, dim, weight, kind, eps, added ? &total : nullptr, &out, eight ? &s : nullptr, stream); });
+    PyObject *const fields[3] = {o.o, sc.o, t.o};
+    return st == AMAP_OK ? named(normed, fields, 3) : PyLong_FromLong(st);
+}
+
+// norm_grad(x, weight, grad, eps, extra or None, dx or None, dweight or None, workspace or None, stream or None) -> (dx, dweight)
+PyObject *norm_grad(PyObject *const *a, Py_ssize_t n) {
+    amap_heads x, grad, extra, dx;
+    amap_type kind;
+    int64_t need = 0, have = 0;
+    void *stream, *work = nullptr;
+    if (n != 9 || !p_norm_grad || !PyFloat_CheckExact(a[3])) return nullptr;
+    const at::Tensor *const tx = like_rows(a[0], x), *const tw = tx ? weight_of(a[1], *tx, kind) : nullptr;
+    if (!tw || x.type == AMAP_E4M3 || !like_rows(a[2], grad, tx) || grad.type != x.type) return nullptr;
+    const bool more = a[4] != Py_None;
+    if (more && (!like_rows(a[4], extra, tx) || extra.type != x.type)) return nullptr;
+    const int64_t tokens = tx->size(0);
+    const int dim = (int)tx->size(tx->dim() - 1);
+    if (p_norm_grad_room(x.heads, tokens, dim, x.type, &need) != AMAP_OK) return nullptr;
+    if (((a[5] == Py_None || a[6] == Py_None || (need && a[7] == Py_None)) && a[8] != Py_None) || !stream_beside(a[8], *tx, &stream)) return nullptr;
+    Ref d, dw;
+    at::Tensor own;
+    {
+        Making without;
+        d.o = a[5] != Py_None ? again(a[5]) : THPVariable_Wrap(made(tx->sizes(), *tx, tx->scalar_type()));
+        dw.o = a[6] != Py_None ? again(a[6]) : THPVariable_Wrap(made({(int64_t)dim}, *tx, at::kFloat));
+        if (need && a[7] == Py_None) own = made({need}, *tx, at::kByte);
+    }
+    const at::Tensor *const tdw = dw.o ? tensor(dw.o, 1, at::kFloat) : nullptr;
+    if (!d.o || !like_rows(d.o, dx, tx) || dx.type != x.type || !tdw || tdw->size(0) != dim || tdw->device() != tx->device()) return nullptr;
+    if (need) {
+        const at::Tensor *const room = a[7] == Py_None ? &own : tensor(a[7], 1, at::kByte);
+        if (!room || room->device() != tx->device()) return nullptr;
+        work = data<void>(*room);
+        have = room->size(0);
+    }
+    const void *const weight = data<void>(*tw);
+    float *const to = data<float>(*tdw);
+    const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+    const amap_status st = called([&] { return p_norm_grad(&x, tokens, dim, weight, kind, eps, &grad, more ? &extra : nullptr, &dx, to, work, have, stream); });
+    return st == AMAP_OK ? PyTuple_Pack(2, d.o, dw.o) : PyLong_FromLong(st);
+}
+
+// quantize(x, gate or None, tall, out or None, scale or None, stream or None) -> (out, scale)
+PyObject *quantize(PyObject *const *a, Py_ssize_t n) {
+    amap_rows x, gate, out;
+    amap_scales s;
+    int64_t tall;
+    void *stream;
+    if (n != 6 || !p_quantize || !whole(a[2], 1, AMAP_SCALE_BLOCK, &tall) || (a[3] == Py_None) != (a[4] == Py_None)) return nullptr;
+    const at::Tensor *const tx = matrix(a[0], x), *const tg = tx && a[1] != Py_None ? matrix(a[1], gate, tx) : nullptr;
+    if (!tx || (a[1] != Py_None && (!tg || tg->sizes() != tx->sizes())) || (a[3] == Py_None && a[5] != Py_None) || !stream_beside(a[5], *tx, &stream)) return nullptr;
+    const int64_t rows = tx->size(0), columns = tx->size(1), down = (rows + tall - 1) / tall;
+    Ref o(a[3] != Py_None ? again(a[3]) : nullptr), sc(a[3] != Py_None ? again(a[4]) : nullptr);
+    if (a[3] == Py_None) {
+        Making without;
+        make_eight(*tx, tx->sizes(), down, o, sc);
+    }
+    const at::Tensor *const to = o.o && sc.o ? matrix(o.o, out, tx) : nullptr;
+    if (!to || to->sizes() != tx->sizes() || !scales(sc.o, down, blocks_of(columns), *tx, s)) return nullptr;
+    const amap_status st = called([&] { return p_quantize(&x, tg ? &gate : nullptr, rows, columns, (int)tall, &out, &s, stream); });
+    PyObject *const fields[2] = {o.o, sc.o};
+    return st == AMAP_OK ? named(in_eight, fields, 2) : PyLong_FromLong(st);
+}
+
+// gemm_scaled(a, a_scale, w, w_scale, dtype, out or None, stream or None) -> out
+PyObject *gemm_scaled(PyObject *const *a, Py_ssize_t n) {
+    amap_rows x, w, y;
+    amap_scales sx, sw;
+    void *stream;
+    if (n != 7 || !p_gemm_scaled) return nullptr;
+    const at::Tensor *const tx = matrix(a[0], x), *const tw = tx ? matrix(a[2], w, tx) : nullptr;
+    if (!tw || tw->size(1) != tx->size(1) || (a[5] == Py_None && a[6] != Py_None) || !stream_beside(a[6], *tx, &stream)) return nullptr;
+    const int64_t M = tx->size(0), N = tw->size(0), K = tx->size(1);
+    if (!scales(a[1], M, blocks_of(K), *tx, sx) || !scales(a[3], blocks_of(N), blocks_of(K), *tx, sw)) return nullptr;
+    Ref out;
+    if (a[5] != Py_None) {
+        out.o = again(a[5]);
+    } else {
+        if (!THPDtype_Check(a[4])) return nullptr;
+        const at::ScalarType t = reinterpret_cast<THPDtype *>(a[4])->scalar_type;
+        if (t != at::kBFloat16 && t != at::kHalf && t != at::kFloat) return nullptr;
+        Making without;
+        out.o = THPVariable_Wrap(made({M, N}, *tx, t));
+    }
+    const at::Tensor *const ty = out.o ? matrix(out.o, y, tx) : nullptr;
+    if (!ty || ty->size(0) != M || ty->size(1) != N) return nullptr;
+    return result(called([&] { return p_gemm_scaled(&x, &sx, &w, &sw, M, N, K, &y, stream); }), again(out.o));
+}
+
 // A call: what it returns; None where it is not taken, an exception of torch's or C++'s among the reasons (the other way meets it again).
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
 PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -386,9 +591,33 @@ PyObject *library(PyObject *, PyObject *const *a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// rows_library(addresses of amap_norm, amap_norm_grad, amap_norm_grad_workspace, amap_quantize, amap_gemm_scaled; the types of a norm's and of 8-bit rows' answer): streams and devices are
+// those that library() was told of
+PyObject *rows_library(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    void *p[5];
+    bool ok = n == 7;
+    for (int i = 0; ok && i < 5; ++i) ok = address(a[i], &p[i]);
+    for (int i = 5; ok && i < 7; ++i) ok = PyType_Check(a[i]) && PyType_IsSubtype(reinterpret_cast<PyTypeObject *>(a[i]), &PyTuple_Type);
+    if (!ok) {
+        PyErr_SetString(PyExc_TypeError, "five addresses and two types");
+        return nullptr;
+    }
+    Py_INCREF(a[5]);
+    Py_XSETREF(normed, a[5]);
+    Py_INCREF(a[6]);
+    Py_XSETREF(in_eight, a[6]);
+    p_norm = reinterpret_cast<decltype(p_norm)>(p[0]);
+    p_norm_grad = reinterpret_cast<decltype(p_norm_grad)>(p[1]);
+    p_norm_grad_room = reinterpret_cast<decltype(p_norm_grad_room)>(p[2]);
+    p_quantize = reinterpret_cast<decltype(p_quantize)>(p[3]);
+    p_gemm_scaled = reinterpret_cast<decltype(p_gemm_scaled)>(p[4]);
+    Py_RETURN_NONE;
+}
+
 #define AMAP_METHOD(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {AMAP_METHOD("rotary", entry<rotary>), AMAP_METHOD("append", entry<append>), AMAP_METHOD("attend", entry<attend>), AMAP_METHOD("assign", entry<assign>),
-                         AMAP_METHOD("library", library), {nullptr, nullptr, 0, nullptr}};
+                         AMAP_METHOD("norm", entry<norm>), AMAP_METHOD("norm_grad", entry<norm_grad>), AMAP_METHOD("quantize", entry<quantize>), AMAP_METHOD("gemm_scaled", entry<gemm_scaled>),
+                         AMAP_METHOD("library", library), AMAP_METHOD("rows_library", rows_library), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_amap_paged_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

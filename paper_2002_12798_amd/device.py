@@ -219,7 +219,7 @@ def assigned_buffers(requests, n_tokens, like=None) -> Assigned:
 
 class _NoCalls:
     """The extension's functions, none of which takes a call."""
-    assign = rotary = append = attend = staticmethod(lambda *args: None)
+    assign = rotary = append = attend = norm = norm_grad = quantize = gemm_scaled = staticmethod(lambda *args: None)
 
 
 def _native_calls():
@@ -430,11 +430,29 @@ def _norm_weight(weight, x, what):
     return weight.data_ptr(), _ELEMENT[weight.dtype]
 
 
+def _one_device(what, stream, *tensors):
+    """The tensors lie on one device, and a call without a stream of its own on the current one."""
+    at = {t.get_device() for t in tensors if t is not None}
+    if len(at) > 1:
+        raise _refused(what, f"tensors on several devices ({', '.join(f'cuda:{i}' for i in sorted(at))})")
+    if stream is None and at != {_get_device()}:
+        raise _refused(what, f"tensors on cuda:{at.pop()} and a stream of cuda:{_get_device()}")
+
+
+if _native is not _NoCalls:
+    _native.rows_library(*(B.C.cast(getattr(B._L, name), B.C.c_void_p).value for name in ("amap_norm", "amap_norm_grad", "amap_norm_grad_workspace", "amap_quantize",
+                                                                                          "amap_gemm_scaled")), Normed, Eight)
+_native_norm, _native_norm_grad, _native_quantize, _native_gemm_scaled = _native.norm, _native.norm_grad, _native.quantize, _native.gemm_scaled
+
+
 def norm(x, weight, eps=1e-6, residual=None, eight=False, out=None, scale=None, total=None, stream=None) -> Normed:
     """The root mean square norm of x [tokens, dim] or [tokens, heads, dim] (each head by itself), times weight [dim] (x's type or float32): with a residual, of
     total = x + residual, rounded to their type.  eight: out in float8_e4m3fn with a scale for each row's blocks of 128 (x [tokens, dim] only).
     out and total may each be x or residual themselves.  No gradient is recorded: norm_grad makes it."""
     what = "amap_norm"
+    done = _native_norm(x, weight, eps, residual, eight, out, scale, total, stream)
+    if done is not None:
+        return done if type(done) is not int else B._check(done, what)
     a = _heads_or_rows(x, what, "x")
     if x.dtype == torch.float8_e4m3fn or (eight and x.dim() != 2) or (scale is not None and not eight) or (total is not None and residual is None):
         raise _refused(what, "x of 8 bits" if x.dtype == torch.float8_e4m3fn else "eight is for x [tokens, dim]" if eight and x.dim() != 2 else
@@ -452,6 +470,7 @@ def norm(x, weight, eps=1e-6, residual=None, eight=False, out=None, scale=None, 
     d = _heads_or_rows(out, what, "out", x, of)
     s = None if scale is None else _scales(scale, x.size(0), _blocks(dim), what, "scale")
     t = None if total is None else _heads_or_rows(total, what, "total", x)
+    _one_device(what, stream, x, weight, residual, out, scale, total)
     B.amap_norm(a, b, x.size(0), dim, at, kind, eps, t, d, s, current_stream() if stream is None else stream)
     return Normed(out, scale, total)
 
@@ -461,6 +480,9 @@ def norm_grad(x, weight, grad, eps=1e-6, extra=None, dx=None, dweight=None, work
     other ways, added to dx.  dweight [dim] is float32, and the same at every call.  dx may be x, grad or extra themselves.  workspace: a uint8 tensor of
     norm_grad_workspace() bytes, for a program that keeps it; calls that may run at the same time must not be given the same one."""
     what = "amap_norm_grad"
+    done = _native_norm_grad(x, weight, grad, eps, extra, dx, dweight, workspace, stream)
+    if done is not None:
+        return done if type(done) is not int else B._check(done, what)
     a = _heads_or_rows(x, what, "x")
     if x.dtype == torch.float8_e4m3fn:
         raise _refused(what, "x of 8 bits")
@@ -479,6 +501,7 @@ def norm_grad(x, weight, grad, eps=1e-6, extra=None, dx=None, dweight=None, work
     if _on_gpu(dweight, torch.float32, 1, what, "dweight").size(0) != x.size(-1):
         raise _refused(what, f"dweight holds {dweight.size(0)} elements, not {x.size(-1)}", B.AMAP_E_SHAPE)
     have = 0 if workspace is None else _on_gpu(workspace, torch.uint8, 1, what, "workspace").numel()
+    _one_device(what, stream, x, weight, grad, extra, dx, dweight, workspace)
     B.amap_norm_grad(a, x.size(0), x.size(-1), at, kind, eps, b, c, d, dweight.data_ptr(), None if workspace is None else workspace.data_ptr(), have,
                      current_stream() if stream is None else stream)
     return dx, dweight
@@ -493,6 +516,9 @@ def quantize(x, gate=None, tall=1, out=None, scale=None, stream=None) -> Eight:
     """x [rows, columns] in float8_e4m3fn, with a float32 scale for each block of `tall` (1: activations, 128: weights) rows and 128 columns: the block's largest value over
     448.  gate: silu(gate) * x instead (tall 1)."""
     what = "amap_quantize"
+    done = _native_quantize(x, gate, tall, out, scale, stream)
+    if done is not None:
+        return done if type(done) is not int else B._check(done, what)
     a = _matrix(x, what, "x")
     b = None if gate is None else _matrix(gate, what, "gate")
     if gate is not None and gate.shape != x.shape:
@@ -508,7 +534,9 @@ def quantize(x, gate=None, tall=1, out=None, scale=None, stream=None) -> Eight:
     c = _matrix(out, what, "out")
     if out.shape != x.shape:
         raise _refused(what, f"out is {tuple(out.shape)}, not {tuple(x.shape)}", B.AMAP_E_SHAPE)
-    B.amap_quantize(a, b, rows, columns, tall, c, _scales(scale, -(-rows // tall), _blocks(columns), what, "scale"), current_stream() if stream is None else stream)
+    d = _scales(scale, -(-rows // tall), _blocks(columns), what, "scale")
+    _one_device(what, stream, x, gate, out, scale)
+    B.amap_quantize(a, b, rows, columns, tall, c, d, current_stream() if stream is None else stream)
     return Eight(out, scale)
 
 
@@ -516,6 +544,9 @@ def gemm_scaled(a, a_scale, w, w_scale, dtype=torch.bfloat16, out=None, stream=N
     """a [m, k] times w [n, k] transposed, both float8_e4m3fn with the scales that quantize gives (a: tall 1, w: tall 128), summed in 32 bits and rounded once to
     dtype (bfloat16, float16, float32; out's type if there is one).  k is a multiple of 16, and rows begin at multiples of 16 bytes."""
     what = "amap_gemm_scaled"
+    done = _native_gemm_scaled(a, a_scale, w, w_scale, dtype, out, stream)
+    if done is not None:
+        return done if type(done) is not int else B._check(done, what)
     x, y = _matrix(a, what, "a"), _matrix(w, what, "w")
     m, k = a.shape
     n = w.size(0)
@@ -530,5 +561,6 @@ def gemm_scaled(a, a_scale, w, w_scale, dtype=torch.bfloat16, out=None, stream=N
     z = _matrix(out, what, "out")
     if tuple(out.shape) != (m, n):
         raise _refused(what, f"out is {tuple(out.shape)}, not {(m, n)}", B.AMAP_E_SHAPE)
+    _one_device(what, stream, a, a_scale, w, w_scale, out)
     B.amap_gemm_scaled(x, s, y, t, m, n, k, z, current_stream() if stream is None else stream)
     return out
