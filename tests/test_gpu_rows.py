@@ -330,7 +330,39 @@ def test_gemm_scaled(dev, m, n, k):
         _check_product(got, a, sa, w, sw, exact, dtype)
 
 
-@pytest.mark.parametrize("m, n, k", [(1, 130, 272), (20, 500, 528), (300, 260, 400), (1100, 1030, 656)])
+WAYS = {"few rows, 16 x 16": [(5, 300, 1296)], "few rows, 16 x 32": [(16, 6144, 1040)], "few rows, 32 x 32": [(72, 2700, 144), (397, 567, 160)], "tiles of 64 x 16": [(100, 2000, 4112)],
+        "tiles of 64 x 32": [(87, 3512, 400)], "tiles of 64 x 32, four stages": [(183, 2637, 96), (51, 5178, 160)], "tiles of 64 x 64": [(256, 4096, 1040)],
+        "tiles of 64 x 64, four stages": [(200, 3000, 400), (1100, 1030, 656)], "tiles of 128 x 128": [(389, 5003, 2576), (2500, 1100, 400)],
+        "tiles of 256 x 128": [(1500, 5000, 272)], "tiles of 256 x 256": [(2100, 4200, 144), (4357, 4100, 80), (4352, 4352, 128), (4352, 4352, 256), (4352, 4352, 400), (4352, 4103, 512)]}
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_every_way_of_gemm_scaled(dev, way, monkeypatch, capfd):
+    """Each is reached (a trace names it), takes whole and partial tiles, several of them to a workgroup, and gives the same bits at every call."""
+    monkeypatch.setenv("AMAP_PLAN_TRACE", "1")
+    for m, n, k in WAYS[way]:
+        for exact, dtype in ((True, BF16), (False, F16)):
+            a, sa, w, sw = (t.cuda() for t in _operands(m + k, m, n, k, exact))
+            capfd.readouterr()
+            got = dev.gemm_scaled(a, sa, w, sw, dtype=dtype)
+            assert f"amap gemm scaled: {way}, {m} x {n} x {k}" in capfd.readouterr().err
+            _check_product(got, a, sa, w, sw, exact, dtype)
+            assert torch.equal(got.view(torch.int16), dev.gemm_scaled(a, sa, w, sw, dtype=dtype).view(torch.int16))
+
+
+@pytest.mark.parametrize("way, m, n, k", [("few rows, 16 x 16", 1, 500, 1040), ("few rows, 16 x 32", 16, 6144, 1040), ("few rows, 32 x 32", 72, 2700, 144),
+                                          ("tiles of 64 x 32, four stages", 87, 3512, 400), ("tiles of 64 x 64, four stages", 389, 5003, 272), ("tiles of 128 x 128", 2500, 1100, 400)])
+def test_every_way_of_gemm_scaled_to_32_bits(dev, way, m, n, k, monkeypatch, capfd):
+    monkeypatch.setenv("AMAP_PLAN_TRACE", "1")
+    for exact in (True, False):
+        a, sa, w, sw = (t.cuda() for t in _operands(m + k, m, n, k, exact))
+        capfd.readouterr()
+        got = dev.gemm_scaled(a, sa, w, sw, dtype=F32)
+        assert f"amap gemm scaled: {way}, {m} x {n} x {k}" in capfd.readouterr().err
+        _check_product(got, a, sa, w, sw, exact, F32)
+
+
+@pytest.mark.parametrize("m, n, k", [(1, 130, 272), (20, 500, 528), (300, 260, 400), (1100, 1030, 656), (2100, 4203, 144)])
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 def test_gemm_scaled_of_strided_operands(dev, m, n, k, dtype):
     """Rows with other things between them (NaN behind the last k, too), scales in no order, an out with room around it, which stays as it was."""

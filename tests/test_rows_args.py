@@ -110,7 +110,8 @@ def _gemm(**over):
     (dict(a=_rows(AT)), I), (dict(w=_rows(3 * AT)), I), (dict(out=_rows(5 * AT, E4)), I), (dict(m=-1), I), (dict(n=-1), I), (dict(k=-16), I),
     (dict(k=0), U), (dict(k=200), U), (dict(a=_rows(AT + 8, E4)), U), (dict(w=_rows(3 * AT + 8, E4)), U), (dict(a=_rows(AT, E4, 264)), U), (dict(w=_rows(3 * AT, E4, 264)), U),
     (dict(out=_rows(5 * AT + 1, stride=300)), U), (dict(a_scale=_scales(2 * AT + 1)), U), (dict(w_scale=_scales(4 * AT + 1)), U),
-    (dict(m=1 << 31), S), (dict(out=_rows(5 * AT, stride=299)), S), (dict(a=_rows(AT, E4, -256)), S), (dict(w_scale=_scales(4 * AT, -1)), S),
+    (dict(a=_rows(AT, E4, 1 << 24)), U), (dict(w=_rows(3 * AT, E4, 1 << 24)), U), (dict(a_scale=_scales(2 * AT, 1 << 24)), U),
+    (dict(m=(1 << 31) - 1, n=1, out=_rows(5 * AT, stride=1)), U), (dict(m=1 << 31), S), (dict(out=_rows(5 * AT, stride=299)), S), (dict(a=_rows(AT, E4, -256)), S), (dict(w_scale=_scales(4 * AT, -1)), S),
     (dict(out=_rows(AT, stride=300)), A), (dict(out=_rows(3 * AT, stride=300)), A), (dict(out=_rows(2 * AT, stride=300)), A), (dict(out=_rows(4 * AT, stride=300)), A),
 ])
 def test_gemm_scaled(over, status):
