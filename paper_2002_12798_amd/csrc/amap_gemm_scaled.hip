@@ -401,6 +401,11 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void amap_gemm_scaled_large_kerne
         const uint64_t x = reinterpret_cast<uint64_t>(p);
         return reinterpret_cast<const char *>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x));
     };
+    auto to_scalar = [&]() __attribute__((always_inline)) {
+        from_a = scalar(ka);
+        from_w = scalar(kw);
+        asm volatile("s_nop 4" : "+s"(from_a), "+s"(from_w));   // (a load reads a scalar register that a vector instruction has written five wait states later; the compiler does not see these loads)
+    };
     auto load_a = [&](int j, uint32_t stage) __attribute__((always_inline)) { load_to_lds(from_a, a_off[j], stage + 1024u * a_block(j)); };
     auto load_w = [&](int j, uint32_t stage) __attribute__((always_inline)) { load_to_lds(from_w, w_off[j], stage + T::A + 1024u * (wave * NW + j)); };
     auto load_first = [&](int l, uint32_t stage, uint32_t slot) __attribute__((always_inline)) {
@@ -445,8 +450,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void amap_gemm_scaled_large_kerne
             begin_tile();
         else
             next_step();
-        from_a = scalar(ka);
-        from_w = scalar(kw);
+        to_scalar();
 #pragma unroll
         for (int l = 0; l < FIRST; ++l) load_first(l, t * T::STAGE, t);
 #pragma unroll
@@ -513,8 +517,7 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void amap_gemm_scaled_large_kerne
                 landed<FIRST + SECOND>();
             }
             next_step();
-            from_a = scalar(ka);
-            from_w = scalar(kw);
+            to_scalar();
 #pragma unroll
             for (int q = Y; q < X; ++q) multiply(q);
             wait(behind && step == 0);   // the next step's w, scales and first half of A; this one's second half is read
@@ -557,8 +560,10 @@ __global__ __launch_bounds__(64 * T::WAVES, 2) void amap_gemm_scaled_large_kerne
                 for (uint32_t l = 0; l < kLoads; ++l) {
                     const uint32_t at = row + l * kRows;
                     const u32x4 x = lds_read<u32x4>(room + at * kRow + ((chunk ^ (at & (kChunks - 1))) << 4));
+                    // (The next tile's waits count one instruction to each of these; more of them would only wait longer.  Not in inline assembly: the hardware reads a 16-byte store's
+                    // registers for two more instructions, in which the compiler then does not know that it must not write there.)
                     if constexpr (decltype(whole_tile)::value)
-                        asm volatile("global_store_dwordx4 %0, %1, off" ::"v"(to), "v"(x) : "memory");   // (one instruction, which is what the next tile's waits count)
+                        *reinterpret_cast<u32x4_any *>(to) = x;
                     else if (m < g.M)
                         store_left(to, left, x);
                     to += down;

@@ -2,6 +2,8 @@
 //
 // A row is held in registers by 16, 32 or 64 lanes, or by a workgroup of up to 16 wavefronts, in pieces of 16 bytes: read once, its sums over the lanes,
 // scaled, written once.  Bound by the bytes.
+#include <algorithm>
+
 #include "amap_rows.hpp"
 
 using namespace amap_rows_detail;
@@ -43,7 +45,7 @@ __device__ __forceinline__ void over_waves(float (&x)[N], float (*part)[N]) {
 }
 
 // LANES: that hold a row (64: a workgroup of whole wavefronts); U: pieces of a lane
-template <class T, int LANES, int U, bool EIGHT>
+template <class T, int LANES, int U, bool EIGHT, int PAST>
 __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_kernel(const NormArgs a) {
     constexpr int V = kPer<T>;
     __shared__ float part[kMaxWaves][1];
@@ -55,12 +57,12 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
     const char *const x = a.x + token * a.x_token + head * a.x_head;
     u32x4 h[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) h[u] = load_piece<T>(x, (lane + u * lanes) * V, a.dim);
+    for (int u = 0; u < U; ++u) h[u] = load_piece<T, PAST>(x, (lane + u * lanes) * V, a.dim);
     if (a.residual) {
         const char *const r = a.residual + token * a.residual_token + head * a.residual_head;
         u32x4 more[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) more[u] = load_piece<T>(r, (lane + u * lanes) * V, a.dim);
+        for (int u = 0; u < U; ++u) more[u] = load_piece<T, PAST>(r, (lane + u * lanes) * V, a.dim);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float sum[V];
@@ -79,7 +81,7 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
     if (a.total && there) {
         char *const t = a.total + token * a.total_token + head * a.total_head;
 #pragma unroll
-        for (int u = 0; u < U; ++u) store_piece<T>(t, (lane + u * lanes) * V, a.dim, h[u]);
+        for (int u = 0; u < U; ++u) store_piece<T, PAST>(t, (lane + u * lanes) * V, a.dim, h[u]);
     }
     const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(squares[0], a.inverse_dim, a.eps));
     char *const out = a.out + token * a.out_token + head * a.out_head;
@@ -98,11 +100,11 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
             uint32_t word[V / 4];
             eight_bits<V>(y, reciprocal_of(scale), word);
             if (there) {
-                store_eight<V>(out, at, a.dim, word);
+                store_eight<V, PAST>(out, at, a.dim, word);
                 if (lane % kBlockLanes<T> == 0 && at < a.dim) a.scale[token * a.scale_row + (int64_t)(at / kBlock) * a.scale_block] = scale;
             }
         } else {
-            if (there) store_piece<T>(out, at, a.dim, piece_of<T>(y));
+            if (there) store_piece<T, PAST>(out, at, a.dim, piece_of<T>(y));
         }
     }
 }
@@ -131,7 +133,7 @@ __device__ __forceinline__ Place place_of(const GradArgs &a, uint32_t row) {
 }
 
 // A group of LANES takes row after row; what each adds to the weight's gradient stays with the lane that has the column.
-template <class T, int LANES, int U>
+template <class T, int LANES, int U, int PAST>
 __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_grad_kernel(const GradArgs a) {
     constexpr int V = kPer<T>;
     constexpr uint32_t kGroups = LANES == 64 ? 1u : 256u / LANES;
@@ -146,20 +148,44 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[u][e] = 0.f;
     }
-    uint32_t turn = 0;
-    for (uint32_t first = blockIdx.x * kGroups; first < a.rows; first += gridDim.x * kGroups, turn ^= 1u) {
-        const bool there = first + group < a.rows;
-        const Place at = place_of(a, there ? first + group : a.rows - 1u);
+    struct Row {
         u32x4 h[U], g[U], more[U];
+    };
+    auto load = [&](const Place &at) __attribute__((always_inline)) {
+        Row x;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            h[u] = load_piece<T>(at.x, (lane + u * lanes) * V, a.dim);
-            g[u] = load_piece<T>(at.grad, (lane + u * lanes) * V, a.dim);
+            x.h[u] = load_piece<T, PAST>(at.x, (lane + u * lanes) * V, a.dim);
+            x.g[u] = load_piece<T, PAST>(at.grad, (lane + u * lanes) * V, a.dim);
         }
         if (at.extra) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) more[u] = load_piece<T>(at.extra, (lane + u * lanes) * V, a.dim);
+            for (int u = 0; u < U; ++u) x.more[u] = load_piece<T, PAST>(at.extra, (lane + u * lanes) * V, a.dim);
         }
+        return x;
+    };
+    // where there is room for it the next row is on its way while one is worked on
+    constexpr bool AHEAD = U == 1;
+    uint32_t turn = 0, first = blockIdx.x * kGroups;   // (every workgroup has rows)
+    Place at = place_of(a, min(first + group, a.rows - 1u));
+    Row row;
+    if constexpr (AHEAD) row = load(at);
+    for (; first < a.rows; first += gridDim.x * kGroups, turn ^= 1u) {
+        const bool there = first + group < a.rows;
+        const uint32_t next = first + gridDim.x * kGroups;
+        Row now;
+        Place place = at;
+        if constexpr (AHEAD) {
+            now = row;
+            if (next < a.rows) {
+                at = place_of(a, min(next + group, a.rows - 1u));
+                row = load(at);
+            }
+        } else {
+            now = load(at);
+            if (next < a.rows) at = place_of(a, min(next + group, a.rows - 1u));
+        }
+        const u32x4(&h)[U] = now.h, (&g)[U] = now.g, (&more)[U] = now.more;
         float sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -180,10 +206,10 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
             for (int e = 0; e < V; ++e) {
                 const float f = element<T>(h[u], e), ge = element<T>(g[u], e);
                 d[e] = r * __builtin_fmaf(-f, along, ge * w[u][e]);
-                if (at.extra) d[e] += element<T>(more[u], e);
+                if (place.extra) d[e] += element<T>(more[u], e);
                 if (there) dw[u][e] = __builtin_fmaf(ge * f, r, dw[u][e]);
             }
-            if (there) store_piece<T>(at.dx, (lane + u * lanes) * V, a.dim, piece_of<T>(d));
+            if (there) store_piece<T, PAST>(place.dx, (lane + u * lanes) * V, a.dim, piece_of<T>(d));
         }
     }
     if constexpr (LANES < 64) {   // the groups' sums in their order
@@ -259,23 +285,31 @@ __global__ __launch_bounds__(64 * kMaxWaves) void amap_norm_grad_wide_kernel(con
             if (c + e < a.dim) to[c + e] = column[c + e];
 }
 
-// dweight = the sum of the workgroups' parts, in their order: 16 lanes of four columns, 16 sets of parts
+// dweight = the sum of the workgroups' parts, in their order: four lanes of four columns, 64 sets of parts
 __global__ __launch_bounds__(256) void amap_norm_join_kernel(const float *parts, uint32_t count, uint32_t pitch, uint32_t dim, float *dw) {
-    __shared__ float sums[16][64];
-    const uint32_t lane = threadIdx.x & 15u, set = threadIdx.x >> 4, at = blockIdx.x * 64u + 4u * lane;
+    __shared__ float sums[64][16];
+    const uint32_t lane = threadIdx.x & 3u, set = threadIdx.x >> 2, at = blockIdx.x * 16u + 4u * lane;
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    if (at < dim)   // (parts are whole fours of columns wide)
-        for (uint32_t i = set; i < count; i += 16) sum += *reinterpret_cast<const f32x4 *>(parts + (size_t)i * pitch + at);
+    if (at < dim) {   // (parts are whole fours of columns wide)
+        constexpr uint32_t U = 4;   // on their way at once
+        const char *const from = reinterpret_cast<const char *>(parts + at);
+        for (uint32_t i = set; i < count; i += 64 * U) {
+            f32x4 x[U];
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u) x[u] = i + 64 * u < count ? *reinterpret_cast<const f32x4 *>(from + (size_t)(i + 64 * u) * pitch * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u) sum += x[u];
+        }
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sums[set][4 * lane + e] = sum[e];
     __syncthreads();
-    const uint32_t column = blockIdx.x * 64u + threadIdx.x;
-    if (threadIdx.x >= 64 || column >= dim) return;
-    float x = 0.f;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) x += sums[k][threadIdx.x];
-    dw[column] = x;
+    // 16 lanes to a column, four sets each
+    const uint32_t column = threadIdx.x >> 4, first = threadIdx.x & 15u;
+    float x = (sums[first][column] + sums[first + 16][column]) + (sums[first + 32][column] + sums[first + 48][column]);
+    x = sum_over<16>(x);
+    if (first == 0 && blockIdx.x * 16u + column < dim) dw[blockIdx.x * 16u + column] = x;
 }
 
 // ---- host
@@ -293,7 +327,8 @@ Held held(uint64_t rows, uint32_t dim, int per, bool eight, uint32_t most_each) 
         h.grid = (uint32_t)((rows * h.lanes + 255) / 256);
         return h;
     }
-    // few rows by as many lanes as there are pieces, many by lanes of several
+    // Few rows by as many lanes as there are pieces, many by lanes of several: the norm, us by pieces of a lane, bf16 16391 rows of 4096 with residual into 8 bits 1 83.3, 2 78.4, 4 78.2,
+    // 2048 rows 1 13.5, 2 12.6, 4 13.3, 60000 rows of 1000 alone 1 44.5, 2 41.0, 4 44.9; fp32 3000 rows of 4096 1 18.1, 2 16.5, 4 16.3, 8 17.1.
     h.each = most_each;
     while (h.each > 1 && (uint64_t)rows * ((pieces + 64 * h.each - 1) / (64 * h.each)) < 4096) h.each /= 2;
     while ((pieces + 64 * h.each - 1) / (64 * h.each) > kMaxWaves) h.each *= 2;
@@ -302,20 +337,30 @@ Held held(uint64_t rows, uint32_t dim, int per, bool eight, uint32_t most_each) 
     return h;
 }
 
-template <class T, bool EIGHT>
-hipError_t norm_of(const Held &h, const NormArgs &g, hipStream_t s) {
+template <class T, bool EIGHT, int PAST>
+hipError_t norm_by(const Held &h, const NormArgs &g, hipStream_t s) {
     const dim3 grid(h.grid), threads(h.threads);
     if constexpr (kBlockLanes<T> == 16 || !EIGHT)
-        if (h.lanes == 16) return launch_kernel<amap_norm_kernel<T, 16, 1, EIGHT>>(grid, threads, 0, s, g);
-    if (h.lanes == 32) return launch_kernel<amap_norm_kernel<T, 32, 1, EIGHT>>(grid, threads, 0, s, g);
-    if (h.each == 1) return launch_kernel<amap_norm_kernel<T, 64, 1, EIGHT>>(grid, threads, 0, s, g);
-    if (h.each == 2) return launch_kernel<amap_norm_kernel<T, 64, 2, EIGHT>>(grid, threads, 0, s, g);
+        if (h.lanes == 16) return launch_kernel<amap_norm_kernel<T, 16, 1, EIGHT, PAST>>(grid, threads, 0, s, g);
+    if (h.lanes == 32) return launch_kernel<amap_norm_kernel<T, 32, 1, EIGHT, PAST>>(grid, threads, 0, s, g);
+    if (h.each == 1) return launch_kernel<amap_norm_kernel<T, 64, 1, EIGHT, PAST>>(grid, threads, 0, s, g);
+    if (h.each == 2) return launch_kernel<amap_norm_kernel<T, 64, 2, EIGHT, PAST>>(grid, threads, 0, s, g);
     if constexpr (T::bytes == 4)
-        if (h.each == 8) return launch_kernel<amap_norm_kernel<T, 64, 8, EIGHT>>(grid, threads, 0, s, g);
-    return launch_kernel<amap_norm_kernel<T, 64, 4, EIGHT>>(grid, threads, 0, s, g);
+        if (h.each == 8) return launch_kernel<amap_norm_kernel<T, 64, 8, EIGHT, PAST>>(grid, threads, 0, s, g);
+    return launch_kernel<amap_norm_kernel<T, 64, 4, EIGHT, PAST>>(grid, threads, 0, s, g);
 }
 template <class T>
-hipError_t grad_of(const Held &h, const GradArgs &g, hipStream_t s) {
+hipError_t norm_of(const Held &h, const NormArgs &g, hipStream_t s) {
+    const bool eight = g.scale != nullptr;
+    const int each = eight ? 1 : T::bytes;
+    const uint64_t stored = reinterpret_cast<uintptr_t>(g.out) | (uint64_t)g.out_token | (uint64_t)g.out_head | g.dim * (uint64_t)each |
+                            (g.total ? reinterpret_cast<uintptr_t>(g.total) | (uint64_t)g.total_token | (uint64_t)g.total_head : 0u);
+    const int past = past_caches((uint64_t)g.rows * g.dim * (T::bytes * (1 + (g.residual != nullptr) + (g.total != nullptr)) + each), stored);
+    if (eight) return past == kBoth ? norm_by<T, true, kBoth>(h, g, s) : past == kStores ? norm_by<T, true, kStores>(h, g, s) : norm_by<T, true, kThrough>(h, g, s);
+    return past == kBoth ? norm_by<T, false, kBoth>(h, g, s) : past == kStores ? norm_by<T, false, kStores>(h, g, s) : norm_by<T, false, kThrough>(h, g, s);
+}
+template <class T, int PAST>
+hipError_t grad_by(const Held &h, const GradArgs &g, hipStream_t s) {
     const dim3 grid(h.grid), threads(h.threads);
     constexpr uint32_t lds = 256 * kPer<T> * 4;
     if (g.dim > kHeldDim) {
@@ -324,12 +369,18 @@ hipError_t grad_of(const Held &h, const GradArgs &g, hipStream_t s) {
         if (e != hipSuccess) return e;
         return launch_kernel<amap_norm_grad_wide_kernel<T>>(grid, threads, (g.dim + kPer<T> - 1) / kPer<T> * kPer<T> * 4u, s, g);
     }
-    if (h.lanes == 16) return launch_kernel<amap_norm_grad_kernel<T, 16, 1>>(grid, threads, lds, s, g);
-    if (h.lanes == 32) return launch_kernel<amap_norm_grad_kernel<T, 32, 1>>(grid, threads, lds, s, g);
-    if (h.each == 1) return launch_kernel<amap_norm_grad_kernel<T, 64, 1>>(grid, threads, 0, s, g);
+    if (h.lanes == 16) return launch_kernel<amap_norm_grad_kernel<T, 16, 1, PAST>>(grid, threads, lds, s, g);
+    if (h.lanes == 32) return launch_kernel<amap_norm_grad_kernel<T, 32, 1, PAST>>(grid, threads, lds, s, g);
+    if (h.each == 1) return launch_kernel<amap_norm_grad_kernel<T, 64, 1, PAST>>(grid, threads, 0, s, g);
     if constexpr (T::bytes == 4)
-        if (h.each == 4) return launch_kernel<amap_norm_grad_kernel<T, 64, 4>>(grid, threads, 0, s, g);
-    return launch_kernel<amap_norm_grad_kernel<T, 64, 2>>(grid, threads, 0, s, g);
+        if (h.each == 4) return launch_kernel<amap_norm_grad_kernel<T, 64, 4, PAST>>(grid, threads, 0, s, g);
+    return launch_kernel<amap_norm_grad_kernel<T, 64, 2, PAST>>(grid, threads, 0, s, g);
+}
+template <class T>
+hipError_t grad_of(const Held &h, const GradArgs &g, hipStream_t s) {
+    const uint64_t stored = reinterpret_cast<uintptr_t>(g.dx) | (uint64_t)g.dx_token | (uint64_t)g.dx_head | (uint64_t)g.dim * T::bytes;
+    const int past = past_caches((uint64_t)g.rows * g.dim * T::bytes * (g.extra ? 4 : 3), stored);
+    return past == kBoth ? grad_by<T, kBoth>(h, g, s) : past == kStores ? grad_by<T, kStores>(h, g, s) : grad_by<T, kThrough>(h, g, s);
 }
 
 bool same_rows(const amap_heads &a, const amap_heads &b, int64_t tokens) {
@@ -355,14 +406,17 @@ amap_status check_sizes(const amap_heads *x, int64_t tokens, int dim, const void
 bool whole_elements(const amap_heads *h) { return !h || reinterpret_cast<uintptr_t>(h->data) % bytes_of(h->type) == 0; }
 const char *const kBegins = "a tensor that does not begin at a whole element";
 
-// workgroups of the gradient's first launch, each of which leaves one part of the weight's
+// Workgroups of the gradient's first launch, each of which leaves one part of the weight's: three rows (or groups of them) to each, up to eight wavefronts to a compute unit.
+// us by workgroups, rows of 4096 in bf16: 512 rows 128 13.4, 256 13.6, 512 17.0   2048 rows 128 28, 256 21.0, 512 22.4   16384 rows 256 97, 512 105, 1024 110;
+// 32768 rows of 1024 512 71.6, 768 57.2, 1024 53.7.  Up to four are left to one workgroup, whose part is the whole: no second launch.
 uint32_t grad_grid(const Held &h) {
-    const uint32_t most = h.threads <= 256 ? 1024 : h.threads <= 512 ? 512 : 256;
-    return h.grid < most ? h.grid : most;
+    const uint32_t waves = h.threads / 64, most = std::max(256u, 2048 / waves);
+    return h.grid <= 4 ? std::min(h.grid, 1u) : std::min(most, (h.grid + 2) / 3);
 }
 uint32_t grad_pitch(int dim) { return ((uint32_t)dim + 3u) / 4u * 4u; }
 Held grad_held(int heads, int64_t tokens, int dim, amap_type type) {
-    Held h = held((uint64_t)tokens * heads, (uint32_t)dim, 16 / bytes_of(type), false, type == AMAP_F32 ? 4 : 2);
+    // one piece to a lane as long as sixteen wavefronts hold a row so: the next row is on its way then (16384 rows of 4096 97 us, by two pieces 105; 32768 of 1024 53.7 and 62)
+    Held h = held((uint64_t)tokens * heads, (uint32_t)dim, 16 / bytes_of(type), false, 1);
     if (dim > (int)kHeldDim) h = Held{64, 64 * kMaxWaves, 1, (uint32_t)(tokens * heads)};
     h.grid = grad_grid(h);
     return h;
@@ -423,14 +477,12 @@ extern "C" amap_status amap_norm(const amap_heads *x, const amap_heads *residual
     g.dim = (uint32_t)head_dim;
     g.eps = eps;
     g.inverse_dim = 1.f / (float)head_dim;
-    const Held h = held(g.rows, g.dim, 16 / es, eight, x->type == AMAP_F32 ? 8 : 4);
+    const Held h = held(g.rows, g.dim, 16 / es, eight, x->type == AMAP_F32 ? 4 : 2);
     if ((uint64_t)h.grid * h.threads >> 32) return refuse("too many rows for one launch");
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const StreamDevice device(s);
     if (device.status() != hipSuccess) return launched(device.status(), "the stream's device");
-    const hipError_t e = x->type == AMAP_F32    ? (eight ? norm_of<F32, true>(h, g, s) : norm_of<F32, false>(h, g, s))
-                         : x->type == AMAP_BF16 ? (eight ? norm_of<Bf16, true>(h, g, s) : norm_of<Bf16, false>(h, g, s))
-                                                : (eight ? norm_of<F16, true>(h, g, s) : norm_of<F16, false>(h, g, s));
+    const hipError_t e = x->type == AMAP_F32 ? norm_of<F32>(h, g, s) : x->type == AMAP_BF16 ? norm_of<Bf16>(h, g, s) : norm_of<F16>(h, g, s);
     return launched(e, "amap_norm_kernel");
 }
 
@@ -506,7 +558,7 @@ extern "C" amap_status amap_norm_grad(const amap_heads *x, int64_t tokens, int h
         if (e != hipSuccess) return launched(e, "amap_norm_grad_kernel");
         if (h.grid == 1) return AMAP_OK;
     }
-    const hipError_t e = launch_kernel<amap_norm_join_kernel>(dim3(((uint32_t)head_dim + 63u) / 64u), dim3(256), 0, s, static_cast<const float *>(workspace), h.grid, g.pitch,
+    const hipError_t e = launch_kernel<amap_norm_join_kernel>(dim3(((uint32_t)head_dim + 15u) / 16u), dim3(256), 0, s, static_cast<const float *>(workspace), h.grid, g.pitch,
                                                               (uint32_t)head_dim, dweight);
     return launched(e, "amap_norm_join_kernel");
 }

@@ -414,10 +414,18 @@ const at::Tensor *weight_of(PyObject *o, const at::Tensor &x, amap_type &type) {
     if (!t || !type_of(t->scalar_type(), type) || (t->scalar_type() != at::kFloat && t->scalar_type() != x.scalar_type())) return nullptr;
     return t->size(0) == x.size(x.dim() - 1) && t->device() == x.device() ? t : nullptr;
 }
-// 8-bit rows and their scales, those of one block of columns beside one another, in one allocation
-void make_eight(const at::Tensor &beside, at::IntArrayRef size, int64_t scale_rows, Ref &out, Ref &scale) {
+// 8-bit rows and their scales, those of one block of columns beside one another, in one allocation; a `total` of the size and type of `beside` there as well, where it is small (0.7 us each)
+void make_eight(const at::Tensor &beside, at::IntArrayRef size, int64_t scale_rows, Ref &out, Ref &scale, Ref *total = nullptr) {
     const int64_t rows = size[0], columns = size[1], blocks = blocks_of(columns), behind = (rows * columns + 15) / 16 * 4;
-    const at::Tensor words = made({behind + scale_rows * blocks}, beside, at::kInt);
+    int64_t words_of = behind + scale_rows * blocks;
+    const int64_t more = (words_of + 3) / 4 * 4, bytes = rows * columns * (int64_t)beside.element_size();
+    const bool small = total && bytes <= 1 << 20;
+    if (small) words_of = more + (bytes + 3) / 4;
+    const at::Tensor words = made({words_of}, beside, at::kInt);
+    if (small)
+        total->o = THPVariable_Wrap(part(words, beside.scalar_type(), size, more * 4 / (int64_t)beside.element_size()));
+    else if (total)
+        total->o = THPVariable_Wrap(made(size, beside, beside.scalar_type()));
     out.o = THPVariable_Wrap(part(words, at::kFloat8_e4m3fn, size, 0));
     at::Tensor s = part(words, at::kFloat, {scale_rows, blocks}, behind);
     const int64_t shape[2] = {scale_rows, blocks}, stride[2] = {1, scale_rows < 1 ? 1 : scale_rows};
@@ -454,11 +462,12 @@ PyObject *norm(PyObject *const *a, Py_ssize_t n) {
             Py_SETREF(sc.o, again(a[6]));
         } else if (eight) {
             Py_CLEAR(sc.o);
-            make_eight(*tx, tx->sizes(), tx->size(0), o, sc);
+            if (make_total) Py_CLEAR(t.o);
+            make_eight(*tx, tx->sizes(), tx->size(0), o, sc, make_total ? &t : nullptr);
         } else {
             o.o = THPVariable_Wrap(made(tx->sizes(), *tx, tx->scalar_type()));
         }
-        if (added) Py_SETREF(t.o, make_total ? THPVariable_Wrap(made(tx->sizes(), *tx, tx->scalar_type())) : again(a[7]));
+        if (added && (!make_total || t.o == Py_None)) Py_SETREF(t.o, make_total ? THPVariable_Wrap(made(tx->sizes(), *tx, tx->scalar_type())) : again(a[7]));
     }
     const int64_t tokens = tx->size(0);
     const int dim = (int)tx->size(tx->dim() - 1);

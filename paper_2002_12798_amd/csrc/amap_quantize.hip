@@ -32,7 +32,7 @@ __device__ __forceinline__ float gated(float gate) {
 
 // Blocks of one row: a block to as many lanes as it has pieces, U blocks beside one another for each of them; the rows of a workgroup follow one another, so that
 // the scales of a column of blocks are written beside one another.
-template <class T, bool GATE, int U>
+template <class T, bool GATE, int U, int PAST>
 __global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeArgs a) {
     constexpr int V = kPer<T>, L = kBlockLanes<T>;
     constexpr uint32_t kRows = kThreads / L;
@@ -46,8 +46,8 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeA
     u32x4 p[U], q[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        p[u] = load_piece<T>(x, first + u * kBlock, left);
-        if constexpr (GATE) q[u] = load_piece<T>(gate, first + u * kBlock, left);
+        p[u] = load_piece<T, PAST>(x, first + u * kBlock, left);
+        if constexpr (GATE) q[u] = load_piece<T, PAST>(gate, first + u * kBlock, left);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -62,13 +62,13 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeA
         const float scale = scale_of(most_over<L>(most));
         uint32_t word[V / 4];
         eight_bits<V>(y, reciprocal_of(scale), word);
-        store_eight<V>(out, at, left, word);
+        store_eight<V, PAST>(out, at, left, word);
         if (lane == 0 && at < left) a.scale[row * a.scale_row + (int64_t)(across * U + u) * a.scale_block] = scale;
     }
 }
 
 // Blocks of 128 rows: one to a workgroup.
-template <class T>
+template <class T, int PAST>
 __global__ __launch_bounds__(kThreads) void amap_quantize_tall_kernel(const QuantizeArgs a) {
     constexpr int V = kPer<T>, L = kBlockLanes<T>, kRows = kThreads / L, U = kBlock / kRows;
     __shared__ float part[kThreads / 64];
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_tall_kernel(const Quan
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t row = first + u * kRows;
-        p[u] = load_piece<T>(x + row * a.x_row, row < a.rows ? at : left, left);
+        p[u] = load_piece<T, PAST>(x + row * a.x_row, row < a.rows ? at : left, left);
     }
     float most = 0.f;
 #pragma unroll
@@ -91,6 +91,8 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_tall_kernel(const Quan
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) most = fmaxf(most, part[w]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) asm volatile("" : "+v"(p[u]));   // (else the elements stay in 32 bits: 84 registers of bf16, and five workgroups to a compute unit instead of eight)
     const float scale = scale_of(most), by = reciprocal_of(scale);
     if (threadIdx.x == 0) a.scale[down * a.scale_row + across * a.scale_block] = scale;
 #pragma unroll
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_tall_kernel(const Quan
         for (int e = 0; e < V; ++e) y[e] = element<T>(p[u], e);
         uint32_t word[V / 4];
         eight_bits<V>(y, by, word);
-        if (row < a.rows) store_eight<V>(a.out + column + row * a.out_row, at, left, word);
+        if (row < a.rows) store_eight<V, PAST>(a.out + column + row * a.out_row, at, left, word);
     }
 }
 
@@ -120,10 +122,23 @@ hipError_t quantize_of(QuantizeArgs &g, int tall, hipStream_t s, bool &fits) {
     fits = grid < (1u << 24);   // (threads of a launch: 32 bits)
     if (!fits) return hipSuccess;
     const dim3 at((uint32_t)grid), threads(kThreads);
-    if (tall != 1) return launch_kernel<amap_quantize_tall_kernel<T>>(at, threads, 0, s, g);
-    if (g.gate) return each == 2 ? launch_kernel<amap_quantize_kernel<T, true, 2>>(at, threads, 0, s, g) : launch_kernel<amap_quantize_kernel<T, true, 1>>(at, threads, 0, s, g);
-    if (each == 4) return launch_kernel<amap_quantize_kernel<T, false, 4>>(at, threads, 0, s, g);
-    return each == 2 ? launch_kernel<amap_quantize_kernel<T, false, 2>>(at, threads, 0, s, g) : launch_kernel<amap_quantize_kernel<T, false, 1>>(at, threads, 0, s, g);
+    const int past = past_caches((uint64_t)g.rows * g.columns * (T::bytes * (g.gate ? 2 : 1) + 1), reinterpret_cast<uintptr_t>(g.out) | (uint64_t)g.out_row | g.columns);
+    const bool few = each == 1;   // (few rows and blocks: nothing goes past the caches)
+    if (tall != 1)
+        return past == kBoth     ? launch_kernel<amap_quantize_tall_kernel<T, kBoth>>(at, threads, 0, s, g)
+               : past == kStores ? launch_kernel<amap_quantize_tall_kernel<T, kStores>>(at, threads, 0, s, g)
+                                 : launch_kernel<amap_quantize_tall_kernel<T, kThrough>>(at, threads, 0, s, g);
+    if (g.gate) {
+        if (few) return launch_kernel<amap_quantize_kernel<T, true, 1, kThrough>>(at, threads, 0, s, g);
+        return past == kBoth     ? launch_kernel<amap_quantize_kernel<T, true, 2, kBoth>>(at, threads, 0, s, g)
+               : past == kStores ? launch_kernel<amap_quantize_kernel<T, true, 2, kStores>>(at, threads, 0, s, g)
+                                 : launch_kernel<amap_quantize_kernel<T, true, 2, kThrough>>(at, threads, 0, s, g);
+    }
+    if (few) return launch_kernel<amap_quantize_kernel<T, false, 1, kThrough>>(at, threads, 0, s, g);
+    if (each == 2) return launch_kernel<amap_quantize_kernel<T, false, 2, kThrough>>(at, threads, 0, s, g);
+    return past == kBoth     ? launch_kernel<amap_quantize_kernel<T, false, 4, kBoth>>(at, threads, 0, s, g)
+           : past == kStores ? launch_kernel<amap_quantize_kernel<T, false, 4, kStores>>(at, threads, 0, s, g)
+                             : launch_kernel<amap_quantize_kernel<T, false, 4, kThrough>>(at, threads, 0, s, g);
 }
 
 }  // namespace

@@ -13,18 +13,24 @@ typedef u32x4 u32x4_any __attribute__((aligned(1)));
 typedef u32x2 u32x2_any __attribute__((aligned(1)));
 typedef uint32_t u32_any __attribute__((aligned(1)));
 
+enum Past { kThrough = 0, kStores = 1, kBoth = 2 };   // the caches: see past_caches
+
 template <class T>
 constexpr int kPer = 16 / T::bytes;   // elements of a piece
 constexpr int kBlock = AMAP_SCALE_BLOCK;
 template <class T>
 constexpr int kBlockLanes = kBlock / kPer<T>;   // lanes that hold a block, a piece each
 
-// Elements `at` .. of a row of `dim` (2^30 bytes at most): whole pieces in one access, the last one of a row by elements; zeros past it.
-template <class T>
+// Elements `at` .. of a row of `dim` (2^30 bytes at most): whole pieces in one access, the last one of a row by elements; zeros past it.  PAST: not kept in the caches.
+template <class T, int PAST = kThrough>
 __device__ __forceinline__ u32x4 load_piece(const char *row, uint32_t at, uint32_t dim) {
     u32x4 p = {0, 0, 0, 0};
     if (at + kPer<T> <= dim) {
-        p = *reinterpret_cast<const u32x4_any *>(row + at * (uint32_t)T::bytes);
+        const u32x4_any *const from = reinterpret_cast<const u32x4_any *>(row + at * (uint32_t)T::bytes);
+        if constexpr (PAST == kBoth)
+            p = __builtin_nontemporal_load(from);
+        else
+            p = *from;
     } else if (at < dim) {
         const char *const from = row + at * (uint32_t)T::bytes;
         const uint32_t n = dim - at;
@@ -39,11 +45,14 @@ __device__ __forceinline__ u32x4 load_piece(const char *row, uint32_t at, uint32
     }
     return p;
 }
-template <class T>
+template <class T, int PAST = kThrough>
 __device__ __forceinline__ void store_piece(char *row, uint32_t at, uint32_t dim, u32x4 p) {
     char *const to = row + at * (uint32_t)T::bytes;
     if (at + kPer<T> <= dim) {
-        *reinterpret_cast<u32x4_any *>(to) = p;
+        if constexpr (PAST != kThrough)
+            __builtin_nontemporal_store(p, reinterpret_cast<u32x4_any *>(to));
+        else
+            *reinterpret_cast<u32x4_any *>(to) = p;
     } else if (at < dim) {
         const uint32_t n = dim - at;
 #pragma unroll
@@ -153,11 +162,15 @@ __device__ __forceinline__ void eight_bits(const float (&x)[V], float by, uint32
     }
 }
 // `at` .. of a row of `dim` bytes
-template <int V>
+template <int V, int PAST = kThrough>
 __device__ __forceinline__ void store_eight(char *row, uint32_t at, uint32_t dim, const uint32_t (&word)[V / 4]) {
     if (at + V <= dim) {
-        if constexpr (V == 8)
+        if constexpr (V == 8 && PAST != kThrough)
+            __builtin_nontemporal_store(u32x2{word[0], word[1]}, reinterpret_cast<u32x2_any *>(row + at));
+        else if constexpr (V == 8)
             *reinterpret_cast<u32x2_any *>(row + at) = u32x2{word[0], word[1]};
+        else if constexpr (PAST != kThrough)
+            __builtin_nontemporal_store(word[0], reinterpret_cast<u32_any *>(row + at));
         else
             *reinterpret_cast<u32_any *>(row + at) = word[0];
     } else if (at < dim) {
@@ -178,6 +191,15 @@ inline Box box_of(const amap_scales &s, int64_t rows, int64_t blocks) {
     const int64_t extent[2] = {rows, blocks}, stride[2] = {s.row_stride, s.block_stride};
     return amap_cache_detail::box_of(s.data, 4, 2, extent, stride);
 }
+// What a call that moves so many bytes stores, and loads as well, past the caches.  us through them / stored past them / loaded past them as well, total MB read and written, outputs in new
+// memory:
+//   norm with residual into 8 bits   117 24.1/21.0        235 45.6/42.9        345 63.8/60.2/59.5   472 85.0/ - /79.7      norm alone   67 12.5/11.6   134 23.5/20.7   268 46.5/45.7
+//   its gradient                     134 31.1/30.5        268 53.1/52.4        393 72.9/ - /70.0    537 96.5/ - /92.6
+//   into 8 bits behind a gate        211 38.4/37.2        422 73.3/ - /65.4    844 144/ - /127      without   127 21.5/20.3   254 45.9/44.4   508 88.9/ - /81.1
+//   by 128 rows                      125 23.0/19.8        251 48.5/45.7        368 69.5/ - /62.9    503 94.2/ - /85.2
+// (Loaded past them below 300 MB, what a call before has left there is read from memory again: norm alone 67 MB 13.3 -> 19.9, 134 MB 22 -> 31.)  Rows that are no whole 64-byte pieces are
+// stored through the caches: a piece is stored by two instructions there.  `stored`: the addresses and steps of what is stored, or-ed.
+inline int past_caches(uint64_t bytes, uint64_t stored) { return stored % 64 || bytes < (64u << 20) ? kThrough : bytes < 300000000 ? kStores : kBoth; }
 inline int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
 
 }  // namespace amap_rows_detail

@@ -448,7 +448,8 @@ _native_norm, _native_norm_grad, _native_quantize, _native_gemm_scaled = _native
 def norm(x, weight, eps=1e-6, residual=None, eight=False, out=None, scale=None, total=None, stream=None) -> Normed:
     """The root mean square norm of x [tokens, dim] or [tokens, heads, dim] (each head by itself), times weight [dim] (x's type or float32): with a residual, of
     total = x + residual, rounded to their type.  eight: out in float8_e4m3fn with a scale for each row's blocks of 128 (x [tokens, dim] only).
-    out and total may each be x or residual themselves.  No gradient is recorded: norm_grad makes it."""
+    out and total may each be x or residual themselves.  No gradient is recorded: norm_grad makes it.  What is made here in 8 bits lies in one buffer with its scales, and a total of up to
+    1 MB beside it: whoever keeps one keeps the others' memory too, or a clone."""
     what = "amap_norm"
     done = _native_norm(x, weight, eps, residual, eight, out, scale, total, stream)
     if done is not None:
@@ -514,7 +515,7 @@ def norm_grad_workspace(x) -> int:
 
 def quantize(x, gate=None, tall=1, out=None, scale=None, stream=None) -> Eight:
     """x [rows, columns] in float8_e4m3fn, with a float32 scale for each block of `tall` (1: activations, 128: weights) rows and 128 columns: the block's largest value over
-    448.  gate: silu(gate) * x instead (tall 1)."""
+    448.  gate: silu(gate) * x instead (tall 1).  What is made here is one buffer."""
     what = "amap_quantize"
     done = _native_quantize(x, gate, tall, out, scale, stream)
     if done is not None:

@@ -341,13 +341,14 @@ def test_every_way_of_gemm_scaled(dev, way, monkeypatch, capfd):
     """Each is reached (a trace names it), takes whole and partial tiles, several of them to a workgroup, and gives the same bits at every call."""
     monkeypatch.setenv("AMAP_PLAN_TRACE", "1")
     for m, n, k in WAYS[way]:
-        for exact, dtype in ((True, BF16), (False, F16)):
+        for exact, dtype in ((True, BF16), (True, F16), (False, F16)):
             a, sa, w, sw = (t.cuda() for t in _operands(m + k, m, n, k, exact))
             capfd.readouterr()
             got = dev.gemm_scaled(a, sa, w, sw, dtype=dtype)
             assert f"amap gemm scaled: {way}, {m} x {n} x {k}" in capfd.readouterr().err
             _check_product(got, a, sa, w, sw, exact, dtype)
-            assert torch.equal(got.view(torch.int16), dev.gemm_scaled(a, sa, w, sw, dtype=dtype).view(torch.int16))
+            for _ in range(20):
+                assert torch.equal(got.view(torch.int16), dev.gemm_scaled(a, sa, w, sw, dtype=dtype).view(torch.int16))
 
 
 @pytest.mark.parametrize("way, m, n, k", [("few rows, 16 x 16", 1, 500, 1040), ("few rows, 16 x 32", 16, 6144, 1040), ("few rows, 32 x 32", 72, 2700, 144),
@@ -399,6 +400,61 @@ def test_gemm_scaled_special_values(dev, m, n, k):
     assert np.isnan(got[-1]).all() and np.isnan(got[:, 5]).all()
     if m > 1:
         assert not np.isfinite(np.delete(got[0], 5)).any()
+
+
+# ---- sizes that go past the caches
+
+def _rows_of(seed, rows, columns, dtype, std=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.empty((rows, columns), dtype=dtype, device="cuda")
+    for part in x.split(4096):
+        part.copy_(torch.randn(part.shape, device="cuda", generator=g) * std)
+    return x
+
+
+@pytest.mark.parametrize("rows", [4100, 16391])
+def test_large_norm(dev, rows):
+    """Stored past the caches, and loaded so as well: every 37th row, and all scales against those of the same rows by themselves (whose squares may be summed in another order: both are
+    within SCALE of the definition's)."""
+    x, r, w = _rows_of(1, rows, 4096, BF16), _rows_of(2, rows, 4096, BF16, 3.0), _rand(3, (4096,), BF16).cuda()
+    h = (x.float() + r.float()).to(BF16)
+    got, wide = dev.norm(x, w, EPS, residual=r, eight=True), dev.norm(x, w, EPS, residual=r)
+    assert torch.equal(got.total, h) and torch.equal(wide.total, h)
+    at = torch.arange(0, rows, 37, device="cuda")
+    y = oracle.norm(_f64(h[at]), _f64(w), EPS)
+    _check_eight(got.out[at], got.scale[at], y, 1)
+    _rounded(wide.out[at], y, NORM, BF16)
+    for part in torch.arange(rows, device="cuda").split(1000):
+        few = dev.norm(h[part], w, EPS, eight=True)
+        _close(_f64(got.scale[part]), _f64(few.scale), 2 * SCALE * (1 + SCALE) * _f64(few.scale))
+
+
+@pytest.mark.parametrize("rows, dtype", [(5000, BF16), (12800, BF16), (9000, F32)])
+def test_large_norm_grad(dev, rows, dtype):
+    x, g, e, w = _rows_of(1, rows, 4096, dtype), _rows_of(2, rows, 4096, dtype, 0.1), _rows_of(3, rows, 4096, dtype, 0.1), _rand(3, (4096,), dtype).cuda()
+    got = dev.norm_grad(x, w, g, EPS, extra=e)
+    dw, mass = torch.zeros(4096, dtype=torch.float64, device="cuda"), torch.zeros(4096, dtype=torch.float64, device="cuda")
+    for a, b in zip(x.split(1000), g.split(1000)):
+        t = b.double() * a.double() / torch.sqrt(a.double().square().mean(-1, keepdim=True) + EPS)
+        dw += t.sum(0)
+        mass += t.abs().sum(0)
+    _close(_f64(got[1]), _f64(dw), (70 + rows) * U * _f64(mass))
+    at = torch.arange(0, rows, 41, device="cuda")
+    dx, _, (own, common), _ = oracle.norm_grad(_f64(x[at]), _f64(w), _f64(g[at]), EPS, _f64(e[at]))
+    off = 40 * U * own + 160 * U * common + 2 * U * np.abs(dx)
+    _close(_f64(got[0][at]), dx, HALF_STEP[dtype] * (np.abs(dx) + off) + off + SMALLEST[dtype])
+
+
+@pytest.mark.parametrize("rows, columns, gate, tall", [(8192, 10240, False, 1), (8192, 10240, True, 1), (6000, 4096, False, 1), (8192, 10240, False, 128), (12000, 4032, False, 128), (30000, 4100, False, 1)])
+def test_large_quantize(dev, rows, columns, gate, tall):
+    x = _rows_of(rows, rows, columns * (1 + gate), BF16)
+    a, b = (x[:, columns:], x[:, :columns]) if gate else (x, None)
+    got = dev.quantize(a, gate=b, tall=tall)
+    step = 128 * tall
+    for first in (0, (rows // 2) // step * step, (rows - 1) // step * step):
+        part = slice(first, min(first + max(tall, 3), rows))
+        y = _f64(a[part]) if b is None else oracle.gated(_f64(a[part]), _f64(b[part]))
+        _check_eight(got.out[part], got.scale[first // tall:-(-part.stop // tall)], y, tall, 36 * U, 17 * U)
 
 
 # ---- together

@@ -50,7 +50,7 @@ def test_norm(over, status):
 
 
 def _grad(**over):
-    c = dict(x=_heads(), tokens=10, dim=200, weight=3 * AT, weight_type=B.AMAP_BF16, eps=1e-6, grad=_heads(2 * AT), extra=_heads(4 * AT), dx=_heads(5 * AT), dweight=6 * AT,
+    c = dict(x=_heads(), tokens=50, dim=200, weight=3 * AT, weight_type=B.AMAP_BF16, eps=1e-6, grad=_heads(2 * AT), extra=_heads(4 * AT), dx=_heads(5 * AT), dweight=6 * AT,
              workspace=7 * AT, bytes=1 << 20)
     c.update(over)
     B.amap_norm_grad(*c.values())
@@ -58,7 +58,7 @@ def _grad(**over):
 
 @pytest.mark.parametrize("over, status", [
     (dict(x=None), I), (dict(x=_heads(None)), I), (dict(grad=None), I), (dict(dx=None), I), (dict(dweight=None), I), (dict(weight=None), I), (dict(grad=_heads(2 * AT, B.AMAP_F32)), I),
-    (dict(extra=_heads(4 * AT, B.AMAP_F16)), I), (dict(dx=_heads(5 * AT, E4)), I), (dict(eps=0.0), I), (dict(workspace=None), I), (dict(bytes=B.amap_norm_grad_workspace(1, 10, 200, B.AMAP_BF16) - 1), I),
+    (dict(extra=_heads(4 * AT, B.AMAP_F16)), I), (dict(dx=_heads(5 * AT, E4)), I), (dict(eps=0.0), I), (dict(workspace=None), I), (dict(bytes=B.amap_norm_grad_workspace(1, 50, 200, B.AMAP_BF16) - 1), I),
     (dict(dim=40000), U), (dict(workspace=7 * AT + 8), U), (dict(dweight=6 * AT + 2), U), (dict(dx=_heads(5 * AT + 1)), U),
     (dict(dx=_heads(5 * AT, heads=2)), S), (dict(dx=_heads(5 * AT, token=128)), S), (dict(tokens=1 << 31), S),
     (dict(dx=_heads(AT + 2)), A), (dict(dx=_heads(2 * AT, token=512)), A), (dict(dx=_heads(4 * AT + 64)), A), (dict(dx=_heads(3 * AT)), A), (dict(dweight=3 * AT), A),
@@ -70,10 +70,10 @@ def test_norm_grad(over, status):
 
 
 def test_what_workspace_the_gradient_takes():
-    """None for a single row, a part for each workgroup else; as much for more rows, up to a bound."""
+    """None for rows that one workgroup takes, a part for each workgroup else; as much for more rows, up to a bound."""
     room = B.amap_norm_grad_workspace
-    assert room(1, 0, 4096, B.AMAP_BF16) == room(1, 1, 4096, B.AMAP_BF16) == 0
-    assert room(1, 2, 4095, B.AMAP_BF16) == 2 * 4096 * 4
+    assert room(1, 0, 4096, B.AMAP_BF16) == room(1, 1, 4096, B.AMAP_BF16) == room(1, 4, 4096, B.AMAP_BF16) == room(1, 32, 200, B.AMAP_BF16) == 0
+    assert room(1, 6, 4095, B.AMAP_BF16) == 2 * 4096 * 4
     assert room(1, 10 ** 7, 4096, B.AMAP_BF16) == room(1, 10 ** 6, 4096, B.AMAP_BF16) <= 1024 * 4096 * 4
     for args, status in (((0, 1, 1, B.AMAP_BF16), I), ((1, -1, 1, B.AMAP_BF16), I), ((1, 1, 1, E4), I), ((1, 1, 32769, B.AMAP_F32), U), ((2, 1 << 30, 64, B.AMAP_F32), S)):
         _refuses(status, room, *args)
