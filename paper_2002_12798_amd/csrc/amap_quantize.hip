@@ -1,5 +1,5 @@
 // Rows and weights into 8 bits with a scale for each block (amap_quantize): every block is read once, held in registers while the lanes that hold it
-// agree on its largest value, and written once.  Bound by the bytes: bf16 8192 x 10240 behind a gate 64.0 us (422 MB, 6.6 TB/s), 6100 x 4080 by 128 rows 16.9 us (75 MB, 4.4), 64 x 2560
+// agree on its largest value, and written once.  Bound by the bytes: bf16 8192 x 10240 behind a gate 64 to 65 us (422 MB, 6.5 TB/s), 6100 x 4080 by 128 rows 14.2 us (75 MB, 5.3), 64 x 2560
 // 2.7 us in the kernel, 5.1 a call.
 #include "amap_rows.hpp"
 
@@ -19,6 +19,7 @@ struct QuantizeArgs {
     int64_t scale_row, scale_block;
     uint32_t rows, columns, across;     // across: workgroups along a row
     FastDiv by_across;
+    bool neighbours;   // blocks beside one another to one XCD
 };
 
 // gate / (1 + exp(-gate)), by exp(-|gate|): neither overflows nor loses what is small.  The product with 1 / ln 2 is carried in two parts, so that the power of two
@@ -73,7 +74,8 @@ template <class T, int PAST>
 __global__ __launch_bounds__(kThreads) void amap_quantize_tall_kernel(const QuantizeArgs a) {
     constexpr int V = kPer<T>, L = kBlockLanes<T>, kRows = kThreads / L, U = kBlock / kRows;
     __shared__ float part[kThreads / 64];
-    const uint32_t down = fdiv(blockIdx.x, a.by_across), across = blockIdx.x - down * a.across;
+    const uint32_t block = a.neighbours ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x;
+    const uint32_t down = fdiv(block, a.by_across), across = block - down * a.across;
     const uint32_t column = across * kBlock, left = min(a.columns - column, (uint32_t)kBlock), at = threadIdx.x % L * V, first = down * kBlock + threadIdx.x / L;
     const char *const x = a.x + (size_t)column * T::bytes;
     u32x4 p[U];
@@ -124,11 +126,14 @@ hipError_t quantize_of(QuantizeArgs &g, int tall, hipStream_t s, bool &fits) {
     if (!fits) return hipSuccess;
     const dim3 at((uint32_t)grid), threads(kThreads);
     const int past = past_caches((uint64_t)g.rows * g.columns * (T::bytes * (g.gate ? 2 : 1) + 1), reinterpret_cast<uintptr_t>(g.out) | (uint64_t)g.out_row | g.columns);
+    // Blocks beside one another share the lines at their edges where rows are no whole lines, and go to one XCD (6100 x 4080 17.8 us, in turn over all eight 21.3; 20000 x 1040 17.6
+    // and 19.9), through its L2 (16391 x 10240 with rows 20496 bytes apart 93.4 us, past it 102.9); else in turn (8192 x 8192 38.2 us, beside one another 43.2).
+    g.neighbours = tall != 1 && (g.x_row % 128 != 0 || reinterpret_cast<uintptr_t>(g.x) % 128 != 0);
     const bool few = each == 1;   // (few rows and blocks: nothing goes past the caches)
     if (tall != 1)
-        return past == kBoth     ? launch_kernel<amap_quantize_tall_kernel<T, kBoth>>(at, threads, 0, s, g)
-               : past == kStores ? launch_kernel<amap_quantize_tall_kernel<T, kStores>>(at, threads, 0, s, g)
-                                 : launch_kernel<amap_quantize_tall_kernel<T, kThrough>>(at, threads, 0, s, g);
+        return past == kBoth && !g.neighbours ? launch_kernel<amap_quantize_tall_kernel<T, kBoth>>(at, threads, 0, s, g)
+               : past != kThrough ? launch_kernel<amap_quantize_tall_kernel<T, kStores>>(at, threads, 0, s, g)
+                                  : launch_kernel<amap_quantize_tall_kernel<T, kThrough>>(at, threads, 0, s, g);
     if (g.gate) {
         if (few) return launch_kernel<amap_quantize_kernel<T, true, 1, kThrough>>(at, threads, 0, s, g);
         return past == kBoth     ? launch_kernel<amap_quantize_kernel<T, true, 2, kBoth>>(at, threads, 0, s, g)
