@@ -38,7 +38,8 @@ template <class T, bool GATE, int U, int PAST>
 __global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeArgs a) {
     constexpr int V = kPer<T>, L = kBlockLanes<T>;
     constexpr uint32_t kRows = kThreads / L;
-    const uint32_t down = fdiv(blockIdx.x, a.by_across), across = blockIdx.x - down * a.across;
+    const uint32_t block = a.neighbours ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x;
+    const uint32_t down = fdiv(block, a.by_across), across = block - down * a.across;
     const uint32_t lane = threadIdx.x % L, row = down * kRows + threadIdx.x / L;
     if (row >= a.rows) return;   // (whole groups of lanes)
     // (from the workgroup's first column on)
@@ -128,7 +129,8 @@ hipError_t quantize_of(QuantizeArgs &g, int tall, hipStream_t s, bool &fits) {
     const int past = past_caches((uint64_t)g.rows * g.columns * (T::bytes * (g.gate ? 2 : 1) + 1), reinterpret_cast<uintptr_t>(g.out) | (uint64_t)g.out_row | g.columns);
     // Blocks beside one another share the lines at their edges where rows are no whole lines, and go to one XCD (6100 x 4080 17.8 us, in turn over all eight 21.3; 20000 x 1040 17.6
     // and 19.9), through its L2 (16391 x 10240 with rows 20496 bytes apart 93.4 us, past it 102.9); else in turn (8192 x 8192 38.2 us, beside one another 43.2).
-    g.neighbours = tall != 1 && (g.x_row % 128 != 0 || reinterpret_cast<uintptr_t>(g.x) % 128 != 0);
+    // Blocks of one row likewise, but not past the caches (4096 x 4080 12.6 and 13.6, 16391 x 10224 100 and 106; 16391 x 10240 with rows 20496 bytes apart 92.7 and 90.6).
+    g.neighbours = (tall != 1 || past == kThrough) && (g.x_row % 128 != 0 || reinterpret_cast<uintptr_t>(g.x) % 128 != 0);
     const bool few = each == 1;   // (few rows and blocks: nothing goes past the caches)
     if (tall != 1)
         return past == kBoth && !g.neighbours ? launch_kernel<amap_quantize_tall_kernel<T, kBoth>>(at, threads, 0, s, g)
