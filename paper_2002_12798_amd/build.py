@@ -18,7 +18,7 @@ PAGED_CALL = os.path.join(_HERE, "_amap_paged_call" + sysconfig.get_config_var("
 
 SOURCES = ["amap_compose.cpp", "amap_graph.cpp", "amap_layout.cpp", "amap_host.cpp", "amap_plan.cpp", "amap_plan_check.cpp", "amap_kernels.hip",
            "amap_gemm.hip", "amap_gemm_ring.hip", "amap_cache.hip", "amap_rotary.hip", "amap_attend.hip", "amap_norm.hip",
-           "amap_quantize.hip", "amap_gemm_scaled.hip"]
+           "amap_quantize.hip", "amap_scaled_product.hip"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
