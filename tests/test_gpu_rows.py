@@ -457,6 +457,26 @@ def test_large_quantize(dev, rows, columns, gate, tall):
         _check_eight(got.out[part], got.scale[first // tall:-(-part.stop // tall)], y, tall, 36 * U, 17 * U)
 
 
+@pytest.mark.parametrize("rows, columns, apart, gate, tall", [(300, 1000, 0, False, 1), (300, 1000, 0, False, 128), (129, 1288, 1, True, 1), (1, 5000, 0, False, 128), (6100, 4080, 0, False, 128),
+                                                              (4096, 4080, 0, False, 1), (16391, 10240, 8, False, 1), (16391, 10240, 8, False, 128), (9000, 10240, 3, True, 1)])
+def test_quantize_rows_of_no_whole_lines(dev, rows, columns, apart, gate, tall):
+    """Blocks of rows that begin inside a line of 128 bytes are taken in another order, and by 128 rows never loaded past the caches: the same bits as of rows that begin at lines, for every block."""
+    lines = _rows_of(rows, rows, -(-columns // 64) * 64 * (1 + gate), BF16)
+    half = lines.shape[1] // 2
+    a, b = (lines[:, half:half + columns], lines[:, :columns]) if gate else (lines[:, :columns], None)
+    want = dev.quantize(a, gate=b, tall=tall)
+    room = [torch.empty((rows, columns + apart), dtype=BF16, device="cuda")[:, apart:] for _ in range(1 + gate)]
+    for to, of in zip(room, (a, b)):
+        to.copy_(of)
+    out = torch.full((rows, columns), 0xFF, dtype=torch.uint8, device="cuda").view(E4M3)
+    scale = torch.full((-(-columns // 128), -(-rows // tall)), -1.0, device="cuda").t()
+    got = dev.quantize(room[0], gate=room[1] if gate else None, tall=tall, out=out, scale=scale)
+    assert torch.equal(got.out.view(torch.uint8), want.out.view(torch.uint8)) and torch.equal(got.scale, want.scale)
+    part = slice((rows - 1) // tall * tall, rows)
+    y = _f64(a[part]) if b is None else oracle.gated(_f64(a[part]), _f64(b[part]))
+    _check_eight(got.out[part], got.scale[part.start // tall:], y, tall, 36 * U, 17 * U)
+
+
 # ---- together
 
 def test_a_gated_layer(dev):
