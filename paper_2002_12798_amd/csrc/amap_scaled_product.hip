@@ -9,7 +9,7 @@
 //
 // Three kernels, eleven shapes (way_of chooses): few rows of a stream w straight into registers; tiles that wavefronts of their own load into LDS; tiles of 256 rows whose loads are
 // spread between the matrix instructions.  Additions to the running sums are four vector instructions to each matrix instruction, half the time of it: they run beside it, two
-// instructions behind, but cost power (16384 x 8192 x 4096 without them 391 us, with them 439).
+// instructions behind, but not for nothing (16384 x 8192 x 4096 without them 397 us, with them 448).
 #include <algorithm>
 #include <atomic>
 #include <cstdio>
@@ -330,8 +330,9 @@ __device__ __forceinline__ void store_left(char *to, uint32_t left, u32x4 x) {
 // A workgroup goes from tile to tile: behind a tile's last step the next one's first is loaded, and its products begin while the stores of the last are on their way (a workgroup to each tile:
 // 9 us more for each, most of it the stores of all of them at once).  Where no tile is left the last step is loaded again, into a stage that nobody reads, so that what is in flight is
 // always the same.
-// 16384 x 8192 x 4096 439 us (2.50 PFLOP/s), of which the matrix cores are busy 61 % at the 1.77 GHz that the power limit leaves (a step's waits taken out by the turns lowered the clock from 1.88); a
-// library's product with one scale for each operand reaches 2.62 on this card.  With all loads of a step at its end 453 us, without any 406.
+// 16384 x 8192 x 4096 447 us (2.46 PFLOP/s; 439 to 455 by card), the matrix cores busy 63 % of the cycles; a library's product with one scale for each operand, which adds no block sums, 346 on the same
+// card (81 % at the same clock).  Without the additions 397, without reads of fragments 442.  With all loads of a step at its end 453, without any 406 (of 439); one turn a step, its loads
+// spread over all of it, 446 to 457, and 4096 x 4096 x 4096 out of memory 66 us instead of 60.
 template <class T>
 struct Large : T {
     static constexpr uint32_t STAGE = T::A + T::W, SLOTS = 4;   // (scales are read until a step's end, and loaded with its first half)
