@@ -22,14 +22,23 @@ struct QuantizeArgs {
     bool neighbours;   // blocks beside one another to one XCD
 };
 
-// gate / (1 + exp(-gate)), by exp(-|gate|): neither overflows nor loses what is small.  The product with 1 / ln 2 is carried in two parts, so that the power of two
-// has 32 bits whatever the gate.
-__device__ __forceinline__ float gated(float gate) {
-    const float a = -__builtin_fabsf(gate), t = a * 0x1.715476p+0f;
-    const float rest = __builtin_fmaf(a, 0x1.715476p+0f, -t) + a * 0x1.4ae0bf8p-26f;
+// gate / (1 + exp(-gate)) * x.  The exponential's argument, the gate over ln 2, is carried in two parts, so that the power of two has 32 bits whatever the gate.
+// In the order x / (1 + exp(-gate)) * gate no step leaves the range of 32 bits that the value does not leave: from gates of -69 on, where the quotient is at least 2^-100 of x.
+// (The gate enters the exponential as -69 to 200: below that as below, above it the sum is 1 from 18 on.)
+constexpr float kInverseLn2 = 0x1.715476p+0f, kInverseLn2Rest = 0x1.4ae0bf8p-26f, kLn2 = 0x1.62e43p-1f, kLowGate = -69.f;
+__device__ __forceinline__ float gated(float gate, float x) {
+    const float g = __builtin_amdgcn_fmed3f(gate, kLowGate, 200.f), t = g * -kInverseLn2;
+    const float rest = __builtin_fmaf(g, -kInverseLn2Rest, __builtin_fmaf(g, -kInverseLn2, -t));
     float e = __builtin_amdgcn_exp2f(t);
-    e = __builtin_fmaf(e, rest * 0x1.62e43p-1f, e);
-    return gate * (gate < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+    e = __builtin_fmaf(e, rest * kLn2, e);
+    return x * __builtin_amdgcn_rcpf(1.f + e) * gate;
+}
+// The same for gates below -69, where the sum is the exponential itself: exp(gate) as a power of two times a factor of 0.7 to 1.4, so that it may lie far below what 32 bits hold and the
+// value still be an ordinary number.  (Below -400 no x leaves anything.)
+__device__ __forceinline__ float low_gated(float gate, float x) {
+    const float g = fmaxf(gate, -400.f), n = __builtin_rintf(g * kInverseLn2);
+    const float f = __builtin_fmaf(g, kInverseLn2Rest, __builtin_fmaf(g, kInverseLn2, -n));
+    return __builtin_ldexpf(x, (int)n) * __builtin_amdgcn_exp2f(f) * gate;
 }
 
 // Blocks of one row: a block to as many lanes as it has pieces, U blocks beside one another for each of them; the rows of a workgroup follow one another, so that
@@ -55,13 +64,25 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeA
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t at = first + u * kBlock;
-        float y[V], most = 0.f;
+        float y[V], most = 0.f, least = 0.f;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             y[e] = element<T>(p[u], e);
-            if constexpr (GATE) y[e] *= gated(element<T>(q[u], e));
-            most = fmaxf(most, size_of(y[e]));
+            if constexpr (GATE) {
+                const float gate = element<T>(q[u], e);
+                least = fminf(least, gate);
+                y[e] = gated(gate, y[e]);
+            }
         }
+        if (GATE && least < kLowGate) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float gate = element<T>(q[u], e);
+                if (gate < kLowGate) y[e] = low_gated(gate, element<T>(p[u], e));
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) most = fmaxf(most, size_of(y[e]));
         const float scale = scale_of(most_over<L>(most));
         uint32_t word[V / 4];
         eight_bits<V>(y, reciprocal_of(scale), word);
