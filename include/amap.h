@@ -524,7 +524,7 @@ amap_status amap_cache_attend_workspace(const amap_cache *cache, int heads, int6
  * with the residual's addition, its gradient, rows and weights rounded to E4M3 with a scale for each block, and the product of such
  * operands.  An element of 8 bits stands for its value times its block's scale.  Blocks are 128 columns wide, and one row (rows of activations) or 128 rows (weights) tall;
  * at the edges they hold what there is.  The scale of a block is the largest of its finite values' sizes over 448, and at
- * least 2^-126; an element is its value over the scale, rounded to nearest even.  Values that are infinite or NaN are NaN in 8 bits, and leave the
+ * least 2^-126; an element is its value over the scale, a division's quotient in 32 bits, rounded to nearest even.  Values that are infinite or NaN are NaN in 8 bits, and leave the
  * scale and the block's other elements alone.
  * No call allocates, synchronises, or reads device memory on the host.  Refusals as for the calls around the paged cache. */
 #define AMAP_SCALE_BLOCK 128

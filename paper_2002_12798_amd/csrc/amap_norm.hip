@@ -100,12 +100,9 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
 #pragma unroll
         for (int e = 0; e < V; ++e) y[e] = element<T>(h[u], e) * r * w[e];
         if constexpr (EIGHT) {
-            float most = 0.f;
-#pragma unroll
-            for (int e = 0; e < V; ++e) most = fmaxf(most, size_of(y[e]));
-            const float scale = scale_of(most_over<kBlockLanes<T>>(most));
+            const float scale = scale_of(most_over<kBlockLanes<T>>(most_of<V>(y)));
             uint32_t word[V / 4];
-            eight_bits<V>(y, reciprocal_of(scale), word);
+            eight_bits<V>(y, divisor_of(scale), word);
             if (there) {
                 store_eight<V, PAST>(out, at, a.dim, word);
                 if (lane % kBlockLanes<T> == 0 && at < a.dim) a.scale[token * a.scale_row + (int64_t)(at / kBlock) * a.scale_block] = scale;

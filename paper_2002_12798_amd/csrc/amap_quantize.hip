@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeA
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t at = first + u * kBlock;
-        float y[V], most = 0.f, least = 0.f;
+        float y[V], least = 0.f;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             y[e] = element<T>(p[u], e);
@@ -81,11 +81,14 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_kernel(const QuantizeA
                 if (gate < kLowGate) y[e] = low_gated(gate, element<T>(p[u], e));
             }
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) most = fmaxf(most, size_of(y[e]));
+        float most;
+        if constexpr (GATE)
+            most = most_of<V>(y);
+        else
+            most = most_of<T, 1>({p[u]});
         const float scale = scale_of(most_over<L>(most));
         uint32_t word[V / 4];
-        eight_bits<V>(y, reciprocal_of(scale), word);
+        eight_bits<V>(y, divisor_of(scale), word);
         store_eight<V, PAST>(out, at, left, word);
         if (lane == 0 && at < left) a.scale[row * a.scale_row + (int64_t)(across * U + u) * a.scale_block] = scale;
     }
@@ -106,19 +109,15 @@ __global__ __launch_bounds__(kThreads) void amap_quantize_tall_kernel(const Quan
         const uint32_t row = first + u * kRows;
         p[u] = load_piece<T, PAST>(x + row * a.x_row, row < a.rows ? at : left, left);
     }
-    float most = 0.f;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int e = 0; e < V; ++e) most = fmaxf(most, size_of(element<T>(p[u], e)));
-    most = most_over<64>(most);
+    float most = most_over<64>(most_of<T>(p));
     if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = most;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) most = fmaxf(most, part[w]);
 #pragma unroll
     for (int u = 0; u < U; ++u) asm volatile("" : "+v"(p[u]));   // (else the elements stay in 32 bits: 84 registers of bf16, and five workgroups to a compute unit instead of eight)
-    const float scale = scale_of(most), by = reciprocal_of(scale);
+    const float scale = scale_of(most);
+    const Divisor by = divisor_of(scale);
     if (threadIdx.x == 0) a.scale[down * a.scale_row + across * a.scale_block] = scale;
 #pragma unroll
     for (int u = 0; u < U; ++u) {

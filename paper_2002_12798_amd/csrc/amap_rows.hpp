@@ -136,9 +136,18 @@ template <int LANES>
 __device__ __forceinline__ float sum_over(float x) {
     return over_lanes<LANES>(x, [](float a, float b) { return a + b; });
 }
+// (of sizes, which are in the order of their bits: maxima of whole numbers take the other lane's in the same instruction)
 template <int LANES>
 __device__ __forceinline__ float most_over(float x) {
-    return over_lanes<LANES>(x, [](float a, float b) { return fmaxf(a, b); });
+    uint32_t u = __float_as_uint(x);
+    auto from = [](uint32_t v, auto lane) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(lane)::value, 0xF, 0xF, false); };
+    u = max(u, from(u, std::integral_constant<int, 0xB1>{}));
+    u = max(u, from(u, std::integral_constant<int, 0x4E>{}));
+    u = max(u, from(u, std::integral_constant<int, 0x141>{}));
+    u = max(u, from(u, std::integral_constant<int, 0x140>{}));
+    if constexpr (LANES >= 32) u = max(u, (uint32_t)__shfl_xor((int)u, 16));
+    if constexpr (LANES >= 64) u = max(u, (uint32_t)__shfl_xor((int)u, 32));
+    return __uint_as_float(u);
 }
 
 // ---- to 8 bits
@@ -148,17 +157,80 @@ __device__ __forceinline__ float size_of(float x) {
     const float a = __builtin_fabsf(x);
     return a < __builtin_inff() ? a : 0.f;
 }
-__device__ __forceinline__ float scale_of(float most) { return fmaxf(most / 448.f, 0x1p-126f); }
-// A value over a scale, by the scale's reciprocal: up to 1.5 steps of 2^-24 from the quotient, where the rounding to 8 bits takes 2^-4; no finite value of the block
-// comes to 464, from where on the conversion would give NaN, as it does for what is infinite.  (From 2^-126 up, a scale and its reciprocal are normal numbers.)
-__device__ __forceinline__ float reciprocal_of(float scale) { return __builtin_amdgcn_rcpf(scale); }
-// V values times `by`, rounded, side by side
+// The largest size of V values that a scale goes by.  (They are looked at one by one only where one of them is infinite: NaN does not enter a maximum.)
 template <int V>
-__device__ __forceinline__ void eight_bits(const float (&x)[V], float by, uint32_t (&word)[V / 4]) {
+__device__ __forceinline__ float most_of(const float (&x)[V]) {
+    float most = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) most = fmaxf(most, __builtin_fabsf(x[e]));
+    if (most == __builtin_inff()) {
+        most = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) most = fmaxf(most, size_of(x[e]));
+    }
+    return most;
+}
+// The same for pieces as they were loaded: sizes are in the order of their bits, two of 16 to an instruction; infinite ones and NaN come after all others, and are left out one by one.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <class T, int N>
+__device__ __forceinline__ float most_of(const u32x4 (&p)[N]) {
+    constexpr uint32_t kSize = T::bytes == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu, kInfinite = T::bytes == 4 ? 0x7F800000u : std::is_same<T, Bf16>::value ? 0x7F80u : 0x7C00u;
+    uint32_t top = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t size = p[n][i] & kSize;
+            if constexpr (T::bytes == 4)
+                top = max(top, size);
+            else
+                top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, size)));
+        }
+    if constexpr (T::bytes == 2) top = max(top & 0xFFFFu, top >> 16);
+    if (top < kInfinite) return element<T>(u32x4{top, 0, 0, 0}, 0);
+    float most = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) most = fmaxf(most, size_of(element<T>(p[n], e)));
+    return most;
+}
+// (most / 448, rounded to 32 bits, from 2^-126 on: the remainder is a whole number of 2^-143)
+__device__ __forceinline__ float scale_of(float most) {
+    constexpr float kInverse = 1.f / 448.f;
+    const float q = most * kInverse;
+    return fmaxf(__builtin_fmaf(__builtin_fmaf(-q, 448.f, most), kInverse, q), 0x1p-126f);
+}
+// A scale to divide by: a division's quotient, rounded to 32 bits, in three instructions instead of eleven.  From the nearest reciprocal, the remainder of value times reciprocal, which a multiply-add has
+// exactly, makes that the nearest quotient (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor, 1990).  By the hardware's reciprocal alone ties of 8 bits, which one in 2000 numbers of 16 bits over a
+// scale of theirs is, went either way.  Remainders are exact where scales are 2^-64 or more; smaller ones are divided by times 2^64.
+struct Divisor {
+    float scale, reciprocal;
+    bool small;   // the scale is 2^64 of it
+};
+__device__ __forceinline__ Divisor divisor_of(float scale) {
+    Divisor d;
+    d.small = scale < 0x1p-64f;
+    d.scale = d.small ? scale * 0x1p64f : scale;
+    d.reciprocal = 1.f / d.scale;   // (a step of Newton's from the hardware's misses the nearest one for some scales, 0x1.fffffep0 among them)
+    return d;
+}
+// (the remainder with its sign turned: -0 stays -0)
+__device__ __forceinline__ float over(float x, const Divisor &d) {
+    const float q = x * d.reciprocal;
+    return __builtin_fmaf(-__builtin_fmaf(q, d.scale, -x), d.reciprocal, q);
+}
+// V values over a scale, rounded to nearest even, side by side.  No finite value of the block comes to 464, from where on the conversion would give NaN, as it does for what is infinite.
+template <int V>
+__device__ __forceinline__ void eight_bits(float (&x)[V], const Divisor &by, uint32_t (&word)[V / 4]) {
+    if (by.small) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] *= 0x1p64f;
+    }
 #pragma unroll
     for (int i = 0; i < V / 4; ++i) {
-        const int low = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * by, x[4 * i + 1] * by, 0, false);
-        word[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * by, x[4 * i + 3] * by, low, true);
+        const int low = __builtin_amdgcn_cvt_pk_fp8_f32(over(x[4 * i], by), over(x[4 * i + 1], by), 0, false);
+        word[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(over(x[4 * i + 2], by), over(x[4 * i + 3], by), low, true);
     }
 }
 // `at` .. of a row of `dim` bytes
