@@ -552,7 +552,8 @@ amap_status amap_norm(const amap_heads *x, const amap_heads *residual, int64_t t
 
 /* The gradient of y with respect to h and the weight, from h (the norm's input, or its total), and that of y:
  * with r = 1 / sqrt(mean of h^2 + eps) and c = sum_j grad_j weight_j h_j:  dx_j = r (grad_j weight_j - h_j r^2 c / head_dim) + extra_j (extra NULL: 0; what reaches h
- * by other ways), dweight_j = sum over all rows of grad_j h_j r, in 32 bits, the same bits at every call.  x, grad, extra and dx are of one type; dx may be the very rows of x, grad or extra.  workspace:
+ * by other ways), dweight_j = sum over all rows of grad_j h_j r, in 32 bits, the same bits at every call.  A row whose squares sum to more than 3.4e38 has r = 0: its
+ * dx is extra and it adds nothing to dweight (NaN where grad_j weight_j h_j sum to more than that as well).  x, grad, extra and dx are of one type; dx may be the very rows of x, grad or extra.  workspace:
  * amap_norm_grad_workspace bytes, 16-byte aligned; its contents need not be kept, and it overlaps nothing.  A call issues up to two launches (see amap_cache_attend). */
 amap_status amap_norm_grad(const amap_heads *x, int64_t tokens, int head_dim, const void *weight, amap_type weight_type, float eps, const amap_heads *grad,
                            const amap_heads *extra, const amap_heads *dx, float *dweight, void *workspace, int64_t workspace_bytes, void *stream);

@@ -211,7 +211,7 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
                 const float f = element<T>(h[u], e), ge = element<T>(g[u], e);
                 d[e] = r * __builtin_fmaf(-f, along, ge * w[u][e]);
                 if (place.extra) d[e] += element<T>(more[u], e);
-                if (there) dw[u][e] = __builtin_fmaf(ge * f, r, dw[u][e]);
+                if (there) dw[u][e] = __builtin_fmaf(ge, f * r, dw[u][e]);   // (h r is at most the root of the row's length; grad h has no such bound)
             }
             if (there) store_piece<T, PAST>(place.dx, (lane + u * lanes) * V, a.dim, piece_of<T>(d));
         }
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void amap_norm_grad_wide_kernel(con
                 const float f = element<T>(h, e), ge = element<T>(g, e);
                 d[e] = r * __builtin_fmaf(-f, along, ge * w[e]);
                 if (at.extra) d[e] += element<T>(more, e);
-                column[c + e] = __builtin_fmaf(ge * f, r, column[c + e]);
+                column[c + e] = __builtin_fmaf(ge, f * r, column[c + e]);
             }
             store_piece<T>(at.dx, c, a.dim, piece_of<T>(d));
         }
