@@ -202,7 +202,8 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
         sums[0] = sum_over<LANES>(sums[0]);
         sums[1] = sum_over<LANES>(sums[1]);
         if constexpr (LANES == 64) over_waves(sums, part[turn]);   // (two sets: whoever writes this one again has met all who read it at the other's barrier)
-        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(sums[0], a.inverse_dim, a.eps)), along = r * r * sums[1] * a.inverse_dim;
+        // (r^2 by itself may pass 32 bits: a row of zeros, or nearly, and eps below 3e-39)
+        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(sums[0], a.inverse_dim, a.eps)), along = sums[1] * a.inverse_dim * r * r;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float d[V];
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void amap_norm_grad_wide_kernel(con
         sums[0] = sum_over<64>(sums[0]);
         sums[1] = sum_over<64>(sums[1]);
         over_waves(sums, part[turn]);
-        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(sums[0], a.inverse_dim, a.eps)), along = r * r * sums[1] * a.inverse_dim;
+        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(sums[0], a.inverse_dim, a.eps)), along = sums[1] * a.inverse_dim * r * r;
         for (uint32_t c = threadIdx.x * V; c < a.dim; c += blockDim.x * V) {   // (dx may be any of the rows that are read: a lane has read its piece before it writes there)
             const u32x4 h = load_piece<T>(at.x, c, a.dim), g = load_piece<T>(at.grad, c, a.dim);
             u32x4 more = {0, 0, 0, 0};

@@ -113,3 +113,15 @@ def test_large_gradients_beside_large_rows(dev, dim):
     got = dev.norm_grad(x.cuda(), w.cuda(), g.cuda(), EPS)
     assert got[1].isfinite().all()
     _check_grad(got, x, w, g, EPS)
+
+
+@pytest.mark.parametrize("eps", [1e-12, 1e-30, 1e-38, 2e-39, 1e-44])
+@pytest.mark.parametrize("dim", [64, 1001, 17000])
+def test_rows_of_zeros_and_a_small_eps(dev, dim, eps):
+    """1 / eps may pass 32 bits where 1 / sqrt(eps) does not: dx = grad weight / sqrt(eps).  (eps is one of 32 bits.)"""
+    eps = float(np.float32(eps))
+    g, w = _rand(2, (5, dim), F32, 1e-3), _rand(3, (dim,), F32)
+    dx, dw = dev.norm_grad(torch.zeros((5, dim), device="cuda"), w.cuda(), g.cuda(), eps)
+    want = _f64(g) * _f64(w) / np.sqrt(eps)
+    _close(_f64(dx), want, 4 * U * np.abs(want) + SMALLEST[F32])
+    assert (dw == 0).all()
