@@ -543,7 +543,7 @@ typedef struct {
 } amap_scales;
 
 /* Of every row of x (a token's, or one of its heads'): h = x + residual rounded to x's type (residual NULL: h = x), y_j = h_j / sqrt(mean of
- * h^2 + eps) * weight_j.  total = h (if not NULL; needs a residual); out = y, rounded once, in x's type, or in 8 bits where its type is AMAP_E4M3, which takes one
+ * h^2 + eps) * weight_j.  eps > 0.  total = h (if not NULL; needs a residual); out = y, rounded once, in x's type, or in 8 bits where its type is AMAP_E4M3, which takes one
  * head and `scale` (blocks of one row; NULL otherwise).  x, residual and total are of one type (F32, BF16, F16), the weight [head_dim] of that or F32.  out and total may each be the
  * very rows of x or of the residual (the same address, strides and type); otherwise nothing that is written shares an element with anything else.  Squares are summed in 32 bits:
  * a row whose squares sum to more than 3.4e38 counts as one with an infinite element, all of whose finite ones become 0.  head_dim <= 32768. */
@@ -566,7 +566,9 @@ amap_status amap_quantize(const amap_rows *x, const amap_rows *gate, int64_t row
 
 /* out[m, n] = sum over blocks b of a_scale[m, b] * w_scale[n / 128, b] * (sum over k in b of a[m, k] * w[n, k]), rounded once to out's type (F32, BF16, F16).
  * a [M, K] and w [N, K] are E4M3, with scales of blocks of one row and of 128 rows.  Products are summed in 32 bits; where out has 16, each eight of them at neighbouring k
- * by a matrix instruction that leaves out what lies below 2^-13 of the largest of the eight (1.5e-5 of a result in the mean).  K is a multiple of 16; rows of a and w begin at multiples of 16 bytes. */
+ * by a matrix instruction that leaves out what lies below 2^-13 of the largest of the eight: over normally distributed operands 1.5e-5 of the root of the terms' squares, a hundredth of bf16's
+ * rounding of an ordinary result and as much as it for one a hundred times smaller, whose terms have cancelled (an out of F32 has the full sums).  a_scale * w_scale is
+ * a number of 32 bits: below 2^-126 it is held to whole 2^-149, past 3.4e38 it is infinite (and NaN beside a sum of 0).  K is a multiple of 16, and not 0; rows of a and w begin at multiples of 16 bytes. */
 amap_status amap_gemm_scaled(const amap_rows *a, const amap_scales *a_scale, const amap_rows *w, const amap_scales *w_scale, int64_t M, int64_t N, int64_t K,
                              const amap_rows *out, void *stream);
 
