@@ -526,7 +526,8 @@ amap_status amap_cache_attend_workspace(const amap_cache *cache, int heads, int6
  * at the edges they hold what there is.  The scale of a block is the largest of its finite values' sizes over 448, and at
  * least 2^-126; an element is its value over the scale, a division's quotient in 32 bits, rounded to nearest even.  Values that are infinite or NaN are NaN in 8 bits, and leave the
  * scale and the block's other elements alone.
- * No call allocates, synchronises, or reads device memory on the host.  Refusals as for the calls around the paged cache. */
+ * No call allocates, synchronises, or reads device memory on the host.  Refusals as for the calls around the paged cache: tensors that lie between one another's rows, as rows of 8 bits with
+ * their scales behind them, are told apart where their rows are the same number of bytes apart. */
 #define AMAP_SCALE_BLOCK 128
 
 /* A [rows, columns] tensor; strides in elements, the elements of a row side by side. */

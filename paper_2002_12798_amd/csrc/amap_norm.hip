@@ -391,9 +391,13 @@ hipError_t grad_of(const Held &h, const GradArgs &g, hipStream_t s) {
 bool same_rows(const amap_heads &a, const amap_heads &b, int64_t tokens) {
     return a.data == b.data && a.type == b.type && (tokens <= 1 || a.token_stride == b.token_stride) && (a.heads <= 1 || a.head_stride == b.head_stride);
 }
+// (rows of one head each: of any types)
+bool share_any(const amap_heads &a, const amap_heads &b, int64_t tokens, int dim) {
+    return a.heads == 1 && b.heads == 1 ? share(runs_of(a, tokens, dim), runs_of(b, tokens, dim)) : share(a, b, tokens, dim);
+}
 // what is written may be the very rows of what is read, or share nothing with it
 bool clash(const amap_heads &written, const amap_heads *read, int64_t tokens, int dim) {
-    return read && !same_rows(written, *read, tokens) && share(written, *read, tokens, dim);
+    return read && !same_rows(written, *read, tokens) && share_any(written, *read, tokens, dim);
 }
 amap_status check_rows(const amap_heads *h, const amap_heads *like, int64_t tokens, int dim, bool written) {
     if (!h->data || h->type != like->type) return AMAP_E_INVALID;
@@ -448,12 +452,12 @@ extern "C" amap_status amap_norm(const amap_heads *x, const amap_heads *residual
     const Box to = amap_cache_detail::box_of(*out, tokens, head_dim), w = amap_cache_detail::box_of(weight, (int64_t)head_dim * bytes_of(weight_type));
     const Box sum = total ? amap_cache_detail::box_of(*total, tokens, head_dim) : Box{};
     if (clash(*out, x, tokens, head_dim) || clash(*out, residual, tokens, head_dim) || meet(to, w) || meet(sum, w)) return AMAP_E_ALIAS;
-    if (total && (clash(*total, x, tokens, head_dim) || clash(*total, residual, tokens, head_dim) || share(*out, *total, tokens, head_dim))) return AMAP_E_ALIAS;
+    if (total && (clash(*total, x, tokens, head_dim) || clash(*total, residual, tokens, head_dim) || share_any(*out, *total, tokens, head_dim))) return AMAP_E_ALIAS;
     if (eight) {
-        const Box s = amap_rows_detail::box_of(*scale, tokens, blocks_of(head_dim));
-        if (!s.fits || !s.apart) return AMAP_E_SHAPE;
-        if (meet(s, to) || meet(s, sum) || meet(s, w) || meet(s, amap_cache_detail::box_of(*x, tokens, head_dim)) ||
-            (residual && meet(s, amap_cache_detail::box_of(*residual, tokens, head_dim))))
+        const Runs s = runs_of(*scale, tokens, blocks_of(head_dim));
+        if (!s.box.fits || !s.box.apart) return AMAP_E_SHAPE;
+        if (meet(s.box, w) || share(s, runs_of(*out, tokens, head_dim)) || (total && share(s, runs_of(*total, tokens, head_dim))) || share(s, runs_of(*x, tokens, head_dim)) ||
+            (residual && share(s, runs_of(*residual, tokens, head_dim))))
             return AMAP_E_ALIAS;
         if (reinterpret_cast<uintptr_t>(scale->data) % 4) return refuse(kBegins);
     }

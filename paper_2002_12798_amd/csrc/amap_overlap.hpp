@@ -112,4 +112,47 @@ inline bool keys_and_values_share(const amap_cache &c) {
     return meet(box_of(c, c.k), box_of(c, c.v)) && reach(s, 0, (int64_t)(reinterpret_cast<uintptr_t>(c.v) - reinterpret_cast<uintptr_t>(c.k)), es * c.head_dim);
 }
 
+// ---- rows that lie between one another's: 8 bits with their scales behind them, a product beside its operand
+
+inline Box box_of(const amap_rows &r, int64_t rows, int64_t columns) {
+    const int64_t extent[2] = {rows, columns}, stride[2] = {r.row_stride, 1};
+    return box_of(r.data, bytes_of(r.type), 2, extent, stride);
+}
+inline Box box_of(const amap_scales &s, int64_t rows, int64_t blocks) {
+    const int64_t extent[2] = {rows, blocks}, stride[2] = {s.row_stride, s.block_stride};
+    return box_of(s.data, 4, 2, extent, stride);
+}
+
+// A tensor as runs of `width` bytes, `step` apart.
+struct Runs {
+    Box box;
+    int64_t count = 0, step = 0, width = 0;
+};
+inline Runs runs_of(const amap_rows &r, int64_t rows, int64_t columns) {
+    const Box box = box_of(r, rows, columns);
+    return Runs{box, rows, box.fits && rows > 1 ? r.row_stride * bytes_of(r.type) : 0, box.fits ? columns * bytes_of(r.type) : 0};
+}
+inline Runs runs_of(const amap_heads &h, int64_t tokens, int dim) { return runs_of(amap_rows{h.data, h.type, h.token_stride}, tokens, dim); }   // (of one head)
+inline Runs runs_of(const amap_scales &s, int64_t rows, int64_t blocks) {   // (along the smaller stride, what lies between two scales among them)
+    const bool across = blocks == 1 || (rows > 1 && s.block_stride <= s.row_stride);
+    const int64_t inner = across ? blocks : rows, by = across ? s.block_stride : s.row_stride, outer = across ? rows : blocks;
+    Runs r{box_of(s, rows, blocks), outer, 0, 0};
+    if (!r.box.fits) return r;
+    r.step = outer > 1 ? 4 * (across ? s.row_stride : s.block_stride) : 0;
+    r.width = inner > 1 ? 4 * ((inner - 1) * by + 1) : 4;
+    return r;
+}
+// Whether two tensors whose boxes fit have a byte in common; taken to be so if their boxes meet and their runs are not the same number of bytes apart.
+inline bool share(const Runs &a, const Runs &b) {
+    if (!meet(a.box, b.box)) return false;
+    const int64_t apart = (int64_t)(b.box.first - a.box.first), step = a.count > 1 ? a.step : b.step;
+    if (a.count > 1 && b.count > 1 && a.step != b.step) return true;
+    if (step == 0 || (a.count <= 1 && b.count <= 1)) return -b.width < apart && apart < a.width;
+    // run i of one and j of the other share a byte if -b.width < apart + (j - i) step < a.width
+    int64_t least = floor_of(-b.width - apart, step) + 1, most = -floor_of(apart - a.width, step) - 1;
+    if (least < 1 - a.count) least = 1 - a.count;
+    if (most > b.count - 1) most = b.count - 1;
+    return least <= most;
+}
+
 }  // namespace amap_cache_detail

@@ -179,10 +179,10 @@ extern "C" amap_status amap_quantize(const amap_rows *x, const amap_rows *gate, 
     if (rows > INT32_MAX || columns > INT32_MAX) return AMAP_E_SHAPE;
     if (rows == 0 || columns == 0) return AMAP_OK;
     if (!x->data || !out->data || !scale->data || (gate && !gate->data)) return AMAP_E_INVALID;
-    const Box from = amap_rows_detail::box_of(*x, rows, columns), by = gate ? amap_rows_detail::box_of(*gate, rows, columns) : Box{},
-              to = amap_rows_detail::box_of(*out, rows, columns), sc = amap_rows_detail::box_of(*scale, (rows + tall - 1) / tall, blocks_of(columns));
-    if (!from.fits || (gate && !by.fits) || !to.fits || !to.apart || !sc.fits || !sc.apart) return AMAP_E_SHAPE;
-    if (meet(to, from) || meet(to, by) || meet(sc, from) || meet(sc, by) || meet(sc, to)) return AMAP_E_ALIAS;
+    const Runs from = runs_of(*x, rows, columns), by = gate ? runs_of(*gate, rows, columns) : Runs{}, to = runs_of(*out, rows, columns),
+               sc = runs_of(*scale, (rows + tall - 1) / tall, blocks_of(columns));
+    if (!from.box.fits || (gate && !by.box.fits) || !to.box.fits || !to.box.apart || !sc.box.fits || !sc.box.apart) return AMAP_E_SHAPE;
+    if (share(to, from) || share(to, by) || share(sc, from) || share(sc, by) || share(sc, to)) return AMAP_E_ALIAS;
     const int es = bytes_of(x->type);
     if (reinterpret_cast<uintptr_t>(x->data) % es || (gate && reinterpret_cast<uintptr_t>(gate->data) % es) || reinterpret_cast<uintptr_t>(scale->data) % 4)
         return refuse("a tensor that does not begin at a whole element");

@@ -255,14 +255,6 @@ __device__ __forceinline__ void store_eight(char *row, uint32_t at, uint32_t dim
 
 // ---- host
 
-inline Box box_of(const amap_rows &r, int64_t rows, int64_t columns) {
-    const int64_t extent[2] = {rows, columns}, stride[2] = {r.row_stride, 1};
-    return amap_cache_detail::box_of(r.data, bytes_of(r.type), 2, extent, stride);
-}
-inline Box box_of(const amap_scales &s, int64_t rows, int64_t blocks) {
-    const int64_t extent[2] = {rows, blocks}, stride[2] = {s.row_stride, s.block_stride};
-    return amap_cache_detail::box_of(s.data, 4, 2, extent, stride);
-}
 // What a call that moves so many bytes stores, and loads as well, past the caches.  us through them / stored past them / loaded past them as well, total MB read and written, outputs in new
 // memory:
 //   norm with residual into 8 bits   117 24.1/21.0        235 45.6/42.9        345 63.8/60.2/59.5   472 85.0/ - /79.7      norm alone   67 12.5/11.6   134 23.5/20.7   268 46.5/45.7

@@ -857,10 +857,9 @@ extern "C" amap_status amap_gemm_scaled(const amap_rows *a, const amap_scales *a
     if (K % 16) return refuse("a K that is no multiple of 16");
     if (M == 0 || N == 0) return AMAP_OK;
     if (!a->data || !w->data || !out->data || !a_scale->data || !w_scale->data) return AMAP_E_INVALID;
-    const Box from = amap_rows_detail::box_of(*a, M, K), by = amap_rows_detail::box_of(*w, N, K), to = amap_rows_detail::box_of(*out, M, N),
-              sa = amap_rows_detail::box_of(*a_scale, M, blocks_of(K)), sw = amap_rows_detail::box_of(*w_scale, blocks_of(N), blocks_of(K));
-    if (!from.fits || !by.fits || !sa.fits || !sw.fits || !to.fits || !to.apart) return AMAP_E_SHAPE;
-    if (meet(to, from) || meet(to, by) || meet(to, sa) || meet(to, sw)) return AMAP_E_ALIAS;
+    const Runs from = runs_of(*a, M, K), by = runs_of(*w, N, K), to = runs_of(*out, M, N), sa = runs_of(*a_scale, M, blocks_of(K)), sw = runs_of(*w_scale, blocks_of(N), blocks_of(K));
+    if (!from.box.fits || !by.box.fits || !sa.box.fits || !sw.box.fits || !to.box.fits || !to.box.apart) return AMAP_E_SHAPE;
+    if (share(to, from) || share(to, by) || share(to, sa) || share(to, sw)) return AMAP_E_ALIAS;
     if (reinterpret_cast<uintptr_t>(a->data) % 16 || reinterpret_cast<uintptr_t>(w->data) % 16 || (M > 1 && a->row_stride % 16) || (N > 1 && w->row_stride % 16))
         return refuse("rows that do not begin at multiples of 16 bytes");
     if (reinterpret_cast<uintptr_t>(out->data) % bytes_of(out->type) || reinterpret_cast<uintptr_t>(a_scale->data) % 4 || reinterpret_cast<uintptr_t>(w_scale->data) % 4)
