@@ -510,6 +510,8 @@ def norm_grad(x, weight, grad, eps=1e-6, extra=None, dx=None, dweight=None, work
 
 def norm_grad_workspace(x) -> int:
     """Bytes of workspace that norm_grad takes for such rows."""
+    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3) or x.dtype not in _ELEMENT:
+        raise _refused("amap_norm_grad_workspace", "x is no tensor of 2 or 3 dimensions and a known type")
     return B.amap_norm_grad_workspace(x.size(1) if x.dim() == 3 else 1, x.size(0), x.size(-1), _ELEMENT[x.dtype])
 
 
