@@ -423,7 +423,7 @@ def _scales(t, rows, blocks, what, name):
 
 
 def _norm_weight(weight, x, what):
-    if not isinstance(weight, torch.Tensor) or weight.dtype not in (x.dtype, torch.float32):
+    if not isinstance(weight, torch.Tensor) or _ELEMENT.get(weight.dtype) not in (_ELEMENT[x.dtype], B.AMAP_F32):
         raise _refused(what, f"weight is no tensor of {x.dtype} or torch.float32")
     if _on_gpu(weight, weight.dtype, 1, what, "weight").size(0) != x.size(-1):
         raise _refused(what, f"weight holds {weight.size(0)} elements, not {x.size(-1)}", B.AMAP_E_SHAPE)
