@@ -400,10 +400,10 @@ bool scales(PyObject *o, int64_t rows, int64_t blocks, const at::Tensor &beside,
     return true;
 }
 int64_t blocks_of(int64_t n) { return (n + AMAP_SCALE_BLOCK - 1) / AMAP_SCALE_BLOCK; }
-// The stream of a call on tensors beside this one: a current stream belongs to the current device.
+// The stream of a call on tensors beside this one: a current stream, and the null stream, belong to the current device.
 bool stream_beside(PyObject *o, const at::Tensor &t, void **stream) {
     if (!stream_of(o, stream)) return false;
-    if (o != Py_None) return true;
+    if (o != Py_None && *stream) return true;
     Ref dev(PyObject_CallNoArgs(get_device));
     int64_t n;
     return dev.o && whole(dev.o, t.get_device(), t.get_device(), &n);

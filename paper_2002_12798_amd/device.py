@@ -431,11 +431,11 @@ def _norm_weight(weight, x, what):
 
 
 def _one_device(what, stream, *tensors):
-    """The tensors lie on one device, and a call without a stream of its own on the current one."""
+    """The tensors lie on one device, and a call without a stream of its own, or on the null stream, on the current one: that is whose streams these are."""
     at = {t.get_device() for t in tensors if t is not None}
     if len(at) > 1:
         raise _refused(what, f"tensors on several devices ({', '.join(f'cuda:{i}' for i in sorted(at))})")
-    if stream is None and at != {_get_device()}:
+    if not stream and at != {_get_device()}:
         raise _refused(what, f"tensors on cuda:{at.pop()} and a stream of cuda:{_get_device()}")
 
 
