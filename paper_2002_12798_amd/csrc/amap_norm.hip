@@ -1,11 +1,11 @@
 // The root mean square norm of rows with the residual's addition and the step to 8 bits (amap_norm), and its gradient (amap_norm_grad).
 //
 // A row is held in registers by 16, 32 or 64 lanes, or by a workgroup of up to 16 wavefronts, in pieces of 16 bytes: read once, its squares summed over the lanes (and, by way
-// of LDS, over the wavefronts), scaled, written once.  Bound by the bytes: bf16 16391 rows of 4096 with the residual into 8 bits 77.5 us (472 MB, 6.1 TB/s; an identity copy reaches
-// 6.0), 4111 x 40 heads of 128 inside their projection 14.9 us (84 MB, 5.6), 16 rows of 4096 4.1 us in the kernel, 5.6 a call.
+// of LDS, over the wavefronts), scaled, written once.  Bound by the bytes: bf16 16391 rows of 4096 with the residual into 8 bits 77.6 us (472 MB, 6.1 TB/s; an identity copy reaches
+// 6.0), 4111 x 40 heads of 128 inside their projection 15.0 us (84 MB, 5.6), 16 rows of 4096 4.1 us in the kernel, 5.6 a call.
 // The gradient takes both of a row's sums (of h^2, and of grad weight h) in one pass.  Its columns' sums stay with the lanes that have the columns, workgroup by workgroup, and a second launch
-// adds the workgroups' parts in their order, so that every call gives the same bits: 16384 rows of 4096 with `extra` 91.5 us (537 MB, 5.9 TB/s), 4.5 of them the second launch;
-// fp32 1531 rows of 1001 11.7 us (in two launches).
+// adds the workgroups' parts in their order, so that every call gives the same bits: 16384 rows of 4096 with `extra` 91.6 us (537 MB, 5.9 TB/s), 4.5 of them the second launch;
+// fp32 1531 rows of 1001 11.6 to 12.2 us (3.5 of them the second launch).
 #include <algorithm>
 
 #include "amap_rows.hpp"
@@ -239,7 +239,8 @@ __global__ __launch_bounds__(LANES == 64 ? 64 * kMaxWaves : 256) void amap_norm_
 }
 
 // The same for rows of more than 16 elements to a lane of sixteen wavefronts: a row is read twice (the second time out of the caches), and the columns' sums are
-// kept in LDS, each by the lane that has its column.
+// kept in LDS, each by the lane that has its column.  Bound by one workgroup to a compute unit, which reads, sums and meets before it writes: bf16 3000 rows of 20000 135.5 us (360 MB, 2.7 TB/s),
+// of 32768 218 (590 MB, 2.7); fp32 2000 rows of 20000 with `extra` 166 (640 MB, 3.9).
 template <class T>
 __global__ __launch_bounds__(64 * kMaxWaves) void amap_norm_grad_wide_kernel(const GradArgs a) {
     constexpr int V = kPer<T>;

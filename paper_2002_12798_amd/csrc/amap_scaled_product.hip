@@ -144,7 +144,8 @@ __device__ __forceinline__ void store_tile(const ScaledArgs &g, const f32x4 (&ac
 // A load instruction holds its wavefront until the address unit takes it, and the few matrix instructions of a smaller tile's step do not fill that time: loading is left to
 // wavefronts of their own, which meet the others once a step.  The others have a step's fragments in registers while they read the next step's.  What is left is the chain of a step: a
 // barrier, the latency of the first reads, the matrix instructions.  us a step of 128 k, one tile to a compute unit, operands in L2: 64 x 16 0.16, 64 x 32 0.19, 64 x 64 0.21, 128 x 128 0.37
-// (out of memory 0.20, 0.24, 0.31, 0.50: what a unit has on its way).  64 x 4096 x 6144 9.7 us, 389 x 2576 x 5003 in 32 bits 24, 512 x 4096 x 6144 23.6 (1.1 PFLOP/s).
+// (out of memory 0.20, 0.24, 0.31, 0.50: what a unit has on its way).  With operands out of memory 64 x 4096 x 6144 12.1 us, 389 x 2576 x 5003 in 32 bits 28.3, 512 x 4096 x 6144 23.7 (1.1 PFLOP/s);
+// out of the last-level cache 9.7, 24.2 and 18.9.
 template <class T>
 __global__ __launch_bounds__(64 * (T::WAVES + T::LOAD), 2) void amap_gemm_scaled_tile_kernel(const ScaledArgs g) {
     constexpr int TI = T::TI, TJ = T::TJ, NA = T::NA, NW = T::NW, NS = T::NS, NST = T::NST;
@@ -637,8 +638,8 @@ hipError_t launch_tiles(ScaledArgs &g, hipStream_t s) {
 // ---- few rows of a: w is streamed once, straight into registers
 
 // TM x TN matrix instructions (16 TM rows of a, 16 TN of w) to a workgroup, whose wavefronts take the blocks of k in turn and join their sums in LDS, in their
-// order.  A wavefront has U blocks on their way: as one is used the next is asked for.  Bound by what memory gives, behind a launch and one latency: 1 x 4096 x 4096 5.3 us (17 MB), 8 x 14336 x 4096
-// 15.7 (59 MB, 3.8 TB/s); more rows read a's rows again for every 16 or 32 columns, from L2, and tiles take over (64 x 4096 x 6144 26, tiles of 64 x 32 12.5).
+// order.  A wavefront has U blocks on their way: as one is used the next is asked for.  Bound by what memory gives, behind a launch and one latency: 1 x 4096 x 4096 6.2 us with weights out of memory (17 MB, 2.7 TB/s; 5.3 out of the last-level cache), 8 x 14336 x 4096
+// 15.4 (59 MB, 3.8 TB/s; 13.9); more rows read a's rows again for every 16 or 32 columns, from L2, and tiles take over (64 x 4096 x 6144 26, tiles of 64 x 32 12.5).
 template <int TM_, int TN_, int U_, bool EXACT_>
 struct Few {
     static constexpr int TM = TM_, TN = TN_, U = U_, MOST = 8;   // MOST: wavefronts
@@ -779,9 +780,11 @@ hipError_t launch_few(ScaledArgs &g, hipStream_t s) {
 
 // The ways to run a product, and what each takes: us, `launch` for the launch, the first loads and the last stores, `tile` for a tile, and for every block of k s1 where
 // a unit has one tile and all units have one (s0: the fewer have one the faster each), s2 for two and `more` for each further one; what lies between whole numbers of tiles per
-// unit counts for `up` of the next one; `mb` for a megabyte of operands and product.  Fitted to products of M = 1 .. 16384, N = 16 .. 20000, K = 32 .. 16384 timed on the
+// unit counts for `up` of the next one; `mb` for a megabyte of operands and product.  Fitted by least squares of the logarithm of estimate over time, a product weighted by the square of the
+// best way's time over this one's, to products of M = 1 .. 16384, N = 16 .. 20000, K = 32 .. 16384 timed on the
 // device with operands from memory (5078 with an out of 16 bits, 2709 of 32), each way where it takes up to twice the best one's time.  What the estimates choose is 0.9 %
-// (0.7 %) off the best way in the mean, 7 % (5 %) at the 95th percentile, 38 % (35 %) at the worst.
+// (0.7 %) off the best way in the mean, 7 % (5 %) at the 95th percentile, 38 % (35 %) at the worst.  They count on the 256 units of a whole card; whatever way is taken is right on any number.
+// Whoever changes a kernel times it anew against the others at such sizes, and fits its line again.
 enum Way { FEW_16x16, FEW_16x32, FEW_32x32, TILE_64x16, TILE_64x32, TILE_64x32_4, TILE_64x64, TILE_64x64_4, TILE_128x128, LARGE_256x128, LARGE_256x256, kWays };
 struct Cost {
     float launch, tile, s0, s1, s2, more, up, mb;   // launch 0: not a way for this type

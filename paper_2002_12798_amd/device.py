@@ -447,7 +447,7 @@ _native_norm, _native_norm_grad, _native_quantize, _native_gemm_scaled = _native
 
 def norm(x, weight, eps=1e-6, residual=None, eight=False, out=None, scale=None, total=None, stream=None) -> Normed:
     """The root mean square norm of x [tokens, dim] or [tokens, heads, dim] (each head by itself), times weight [dim] (x's type or float32): with a residual, of
-    total = x + residual, rounded to their type.  eight: out in float8_e4m3fn with a scale for each row's blocks of 128 (x [tokens, dim] only).
+    total = x + residual, rounded to their type (and made here if it is not given).  eps > 0.  eight: out in float8_e4m3fn with a scale for each row's blocks of 128 (x [tokens, dim] only).
     out and total may each be x or residual themselves.  No gradient is recorded: norm_grad makes it.  What is made here in 8 bits lies in one buffer with its scales, and a total of up to
     1 MB beside it: whoever keeps one keeps the others' memory too, or a clone."""
     what = "amap_norm"
@@ -545,7 +545,8 @@ def quantize(x, gate=None, tall=1, out=None, scale=None, stream=None) -> Eight:
 
 def gemm_scaled(a, a_scale, w, w_scale, dtype=torch.bfloat16, out=None, stream=None) -> torch.Tensor:
     """a [m, k] times w [n, k] transposed, both float8_e4m3fn with the scales that quantize gives (a: tall 1, w: tall 128), summed in 32 bits and rounded once to
-    dtype (bfloat16, float16, float32; out's type if there is one).  k is a multiple of 16, and rows begin at multiples of 16 bytes."""
+    dtype (bfloat16, float16, float32; out's type if there is one).  For an out of 16 bits products of eight neighbouring k are summed to 2^-13 of their largest, which shows where a result is a hundred
+    times smaller than its terms; a float32 one has the full sums.  k is a multiple of 16, and rows begin at multiples of 16 bytes."""
     what = "amap_gemm_scaled"
     done = _native_gemm_scaled(a, a_scale, w, w_scale, dtype, out, stream)
     if done is not None:
